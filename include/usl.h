@@ -238,6 +238,67 @@ usl_status usl_redistribute(usl_ctx* ctx, int32_t* idx, void* W, float* m1, floa
 usl_status usl_redistribute_rows(usl_ctx* ctx, int32_t* idx, void* W, float* m1, float* m2,
                                  int32_t per_row, uint64_t seed, uint64_t epoch);
 
+/* ---- Around the layer: the normalisation in front of it, its values in 4 bits, its scores as they are served ----
+ * What follows is not in the paper.  The paper feeds the layer from a trunk and ranks its scores as they are; these calls are
+ * what such a trunk's last step and a server of the predictions need beside the calls above. */
+
+/* Layer norm of rows h[b][d] (storage type) that become the activations x[b][d] (storage type, overwritten; may be h):
+ *   mean = sum_c h / d,  rstd = (sum_c (h - mean)^2 / d + eps)^-1/2,  x = (h - mean) * rstd * gamma + beta
+ * gamma, beta [d] float32, each may be NULL (1 and 0).  mean, rstd [b] float32, results for usl_layer_norm_backward, each
+ * may be NULL.  eps finite and > 0.  Everything is computed in float32 or more and rounded once. */
+usl_status usl_layer_norm(usl_ctx* ctx, const void* h, const float* gamma, const float* beta, float eps, void* x,
+                          float* mean, float* rstd, int32_t b);
+
+/* Its backward pass, from the gradient by x that usl_backward_input, usl_backward and usl_train_step return:
+ *   n = (h - mean) * rstd,  u = grad_x * gamma
+ *   grad_h[i][c]  = rstd * (u - sum_c u / d - n * sum_c (u * n) / d)
+ *   grad_gamma[c] = sum_i grad_x * n,   grad_beta[c] = sum_i grad_x
+ * h, gamma, mean, rstd as the forward call had and left them (gamma may be NULL: 1).  grad_x, grad_h [b][d], grad_gamma,
+ * grad_beta [d] float32, all overwritten; grad_gamma and grad_beta may each be NULL.  grad_h must be neither grad_x nor h.
+ * The sums over the instances are taken in a fixed order: equal calls give equal bits. */
+usl_status usl_layer_norm_backward(usl_ctx* ctx, const float* grad_x, const void* h, const float* gamma, const float* mean,
+                                   const float* rstd, float* grad_h, float* grad_gamma, float* grad_beta, int32_t b);
+
+/* The values in microscaled 4-bit numbers: the slots of a label in blocks of 32, each block with a power of two as its scale.
+ *   scales [m][ceil(k/32)] uint8   byte s stands for 2^(s-127); 255: the block's values are NaN
+ *   codes  [m][ceil(k/8)]  uint32  slot t of a label is bits 4*(t%8) .. 4*(t%8)+3 of word t/8: a sign bit (8) and one of
+ *                                  the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 to 7); codes behind slot k-1 are 0
+ * usl_quantize_mx4: scale 2^(floor(log2 of the block's largest magnitude) - 2), at least 2^-127, and the nearest code to W / scale
+ * (a half between two goes to the even one, beyond 6 to 6).  A block with an infinity or NaN gets scale 255; one of zeros 0.
+ * usl_dequantize_mx4: W [m][k] storage type = code * scale, exactly.  With bfloat16 or float32 weights that are what a call
+ * of it left, usl_quantize_mx4 gives numbers of the same values back. */
+usl_status usl_quantize_mx4(usl_ctx* ctx, const void* W, uint32_t* codes, uint8_t* scales);
+usl_status usl_dequantize_mx4(usl_ctx* ctx, const uint32_t* codes, const uint8_t* scales, void* W);
+
+/* usl_forward with such values in W's place: 4.5 bits a connection instead of 32 or 16, the activations in the storage type
+ * and sums in float32 as there.  (Gradients by x go through usl_backward_input on the values of usl_dequantize_mx4.) */
+usl_status usl_forward_mx4(usl_ctx* ctx, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales,
+                           float* out, int32_t b);
+
+/* What a server does to a score z = out[i][j] before it ranks it.  c is the number of times that j stands in the list of
+ * instance i (labels it has been shown, bought, or answered with already; entries outside [0, m) say nothing):
+ *   c > 0:        z <- (z > 0 ? z / repeat : z * repeat) - (presence + frequency * c)
+ *   bias:         z <- z + bias[j]
+ *   not allowed:  z <- -infinity, whatever it was (NaN too)
+ * Label j is allowed where bit j % 32 of word j / 32 of the instance's mask is set. */
+typedef struct {
+    const float* bias;         /* [m] float32, device; NULL: 0 */
+    const uint32_t* allowed;   /* [allowed_rows][ceil(m/32)], device; NULL: every label is */
+    int32_t allowed_rows;      /* 1 (one mask for all instances) or at least b (one each) */
+    const int64_t* shown_off;  /* [b+1] int64, device, CSR as the targets' offsets; NULL: nothing was shown */
+    const int32_t* shown_lab;  /* [shown_off[b]] int32, device; repeats count */
+    float repeat;              /* finite, > 0; 1: none */
+    float presence, frequency; /* finite; 0: none */
+} usl_adjustments;
+
+/* adjusted [b][m] float32 = out [b][m] after the adjustments; may be out.  adj: host memory, read during the call. */
+usl_status usl_adjust_scores(usl_ctx* ctx, const float* out, const usl_adjustments* adj, float* adjusted, int32_t b);
+
+/* usl_topk of the adjusted scores, which are not written.  Only allowed labels are listed: where fewer than kk are, the ranks behind them
+ * hold label -1 and -infinity.  Scores of allowed labels must not be NaN.  1 <= kk <= min(m, 32). */
+usl_status usl_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk,
+                             int32_t* top_lab, float* top_val);
+
 /* Debug check of the uniform-sparsity invariant (Section 3.2): counts rows of idx that hold a
  * value outside [0, d) or the same column twice.  n_bad_host: host pointer; the call waits. */
 usl_status usl_validate_indices(usl_ctx* ctx, const int32_t* idx, int64_t* n_bad_host);

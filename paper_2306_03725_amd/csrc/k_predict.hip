@@ -13,41 +13,15 @@ constexpr int TK_NT = 256;             // lanes per workgroup
 // scores a lane holds in registers: 64, or 8 where that would leave most of the chip without a workgroup
 constexpr int TK_EPT = 64, TK_EPT_FEW = 8;
 static_assert(TK_NT * TK_EPT_FEW == TOPK_SHORT_SEGMENT, "what the choice of a prediction's path counts with");
-constexpr int TK_MAX = 32;             // largest kk
-
-// Largest v of the workgroup, returned to every lane.  red: two sets used in turn, so one barrier is enough.
-template <int NT>
-struct BlockMax {
-    uint64_t (*red)[NT / 64];
-    int turn;
-    __device__ __forceinline__ uint64_t operator()(uint64_t v) {
-        v = wave_max(v);
-        uint64_t* set = red[turn];
-        turn ^= 1;
-        if ((threadIdx.x & 63) == 0) set[threadIdx.x >> 6] = v;
-        __syncthreads();
-        uint64_t r = set[0];
-#pragma unroll
-        for (int w = 1; w < NT / 64; ++w) r = set[w] > r ? set[w] : r;
-        return r;
-    }
-};
 
 // The kk best keys of one segment of 256 * TK_EPT labels of one row, best first, into cand[row][segment][kk]
-// (0 where the segment has fewer than kk labels).
-//   1. every lane loads its TK_EPT scores (all loads in flight at once) and finds its own best key;
-//   2. tau = the kk-th best of the 256 lane maxima: at least kk keys of the segment are >= tau, and
-//      every key >= tau belongs to one of the kk lanes whose maximum is >= tau, so at most kk*TK_EPT keys pass;
-//   3. those keys are collected in LDS and the best kk are peeled off one by one ("largest key below the
-//      previous winner": keys are distinct, so nothing has to be removed).
+// (0 where the segment has fewer than kk labels): every lane loads its TK_EPT scores, all loads in flight at once (best_of_segment).
 // VEC: rows are 16-byte aligned and m % 4 == 0, so a lane reads groups of 4 consecutive labels.
 template <bool VEC, int TK_EPT>
 __global__ void __launch_bounds__(TK_NT)
 k_topk_segments(const float* __restrict__ out, int64_t m, int kk, int nseg, uint64_t* __restrict__ cand) {
-    __shared__ uint64_t red[2][TK_NT / 64];
-    BlockMax<TK_NT> block_max = {red, 0};
-    __shared__ uint64_t list[TK_MAX * TK_EPT];
-    __shared__ uint32_t count;
+    __shared__ TopkSegment<TK_NT> shared;
+    __shared__ uint64_t list[TOPK_MAX * TK_EPT];
     constexpr int TK_SEG = TK_NT * TK_EPT;   // labels per workgroup
     const int64_t seg0 = (int64_t)blockIdx.x * TK_SEG;
     const float* row = out + (int64_t)blockIdx.y * m + seg0;
@@ -72,45 +46,8 @@ k_topk_segments(const float* __restrict__ out, int64_t m, int kk, int nseg, uint
             v[e] = j < lim ? row[j] : 0.f;
         }
     }
-    // the lane's best score; labels grow with e, so the first of equal scores is the smaller label
-    float top = 0.f;
-    int top_j = -1;
-#pragma unroll
-    for (int e = 0; e < TK_EPT; ++e) {
-        const int j = local_of(e);
-        const bool better = j < lim && (top_j < 0 || v[e] > top);
-        top = better ? v[e] : top;
-        top_j = better ? j : top_j;
-    }
-    const uint64_t mine = top_j >= 0 ? score_key(top, (uint32_t)(seg0 + top_j)) : 0ull;
-    uint64_t tau = ~0ull;
-    for (int r = 0; r < kk && tau != 0; ++r) tau = block_max(mine < tau ? mine : 0ull);
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    // keys are built only for scores that reach tau's score (a cheap float test first)
-    const uint32_t tu = (uint32_t)(tau >> 32);
-    const float tau_score = tau == 0 ? -INFINITY : __uint_as_float((tu & 0x80000000u) ? (tu & 0x7FFFFFFFu) : ~tu);
-#pragma unroll
-    for (int e = 0; e < TK_EPT; ++e) {
-        const int j = local_of(e);
-        if (j < lim && v[e] >= tau_score) {
-            const uint64_t key = score_key(v[e], (uint32_t)(seg0 + j));
-            if (key >= tau) list[atomicAdd(&count, 1u)] = key;
-        }
-    }
-    __syncthreads();
-    const uint32_t n = count;
-    uint64_t* dst = cand + ((size_t)blockIdx.y * nseg + blockIdx.x) * kk;
-    uint64_t prev = ~0ull;
-    for (int r = 0; r < kk; ++r) {
-        uint64_t best = 0;
-        for (uint32_t q = threadIdx.x; q < n; q += TK_NT) {
-            const uint64_t key = list[q];
-            if (key < prev && key > best) best = key;
-        }
-        prev = block_max(best);
-        if (threadIdx.x == 0) dst[r] = prev;
-    }
+    best_of_segment<TK_NT, TK_EPT>(v, local_of, [&](int, int j) -> bool { return j < lim; }, seg0, kk, shared, list,
+                                   cand + ((size_t)blockIdx.y * nseg + blockIdx.x) * kk);
 }
 
 // One workgroup per row: the best kk of the row's nseg*kk candidate keys, unpacked.  A launch of its own: merged by the workgroup
@@ -138,8 +75,8 @@ k_topk_merge(const uint64_t* __restrict__ cand, int n, int kk, int32_t* __restri
         }
         prev = block_max(best);
         if ((int)threadIdx.x == r) {
-            top_lab[(size_t)blockIdx.x * kk + r] = key_label(prev);
-            top_val[(size_t)blockIdx.x * kk + r] = key_score(prev);
+            top_lab[(size_t)blockIdx.x * kk + r] = prev ? key_label(prev) : -1;   // fewer than kk labels are allowed
+            top_val[(size_t)blockIdx.x * kk + r] = prev ? key_score(prev) : -INFINITY;
         }
     }
 }
@@ -163,7 +100,7 @@ k_precision_hits(const int32_t* __restrict__ top_lab, const int64_t* __restrict_
 
 }  // namespace
 
-int usl_topk_max(void) { return TK_MAX; }
+int usl_topk_max(void) { return TOPK_MAX; }
 
 static int topk_segments(const usl_ctx* c, int ept) { return (int)((c->m + TK_NT * ept - 1) / (TK_NT * ept)); }
 
@@ -174,8 +111,8 @@ static int topk_segments(const usl_ctx* c, int ept) { return (int)((c->m + TK_NT
 usl_status usl_reserve_topk(usl_ctx* c) {
     const size_t most = (size_t)topk_segments(c, TK_EPT) * c->max_b, most_few = (size_t)topk_segments(c, TK_EPT_FEW) * (c->num_cu / topk_segments(c, TK_EPT) + 1);
     const size_t by_forward = (size_t)usl_forward_few_blocks(c);
-    const size_t two = most > most_few ? most : most_few;
-    const size_t bytes = (two > by_forward ? two : by_forward) * TK_MAX * 8, had = c->topk_cand_cap;
+    const size_t two = most > most_few ? most : most_few, adjusted = usl_adjusted_segments(c), three = two > adjusted ? two : adjusted;
+    const size_t bytes = (three > by_forward ? three : by_forward) * TOPK_MAX * 8, had = c->topk_cand_cap;
     USL_TRY(usl_reserve(c, (void**)&c->topk_cand, &c->topk_cand_cap, bytes + 64));
     if (had != c->topk_cand_cap) c->topk_done_clear = false;
     c->topk_done = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(c->topk_cand) + bytes);

@@ -32,7 +32,7 @@ extern "C" usl_status usl_destroy(usl_ctx* c) {
     if (c->device >= 0) {
         void* bufs[] = {c->bce_partials, c->sel_hist, c->prune_flags, c->tie_counts, c->counter64,
                         c->csc_ptr, c->csc_cursor, c->csc_order, c->csc_slot, c->csc_w, c->gT, c->gxT, c->nz_flags,
-                        c->slot_order, c->topk_cand, c->sub_idx, c->sub_W, c->predict_out, c->gw_part,
+                        c->slot_order, c->topk_cand, c->sub_idx, c->sub_W, c->predict_out, c->norm_part, c->gw_part,
                         c->nz_state, c->nz_bits, c->nz_lab, c->nz_val, c->idx_print, c->xi, c->xr, c->tgt_bits, c->small_sums, c->small_order};
         (void)hipStreamSynchronize(c->stream);
         for (void* p : bufs)
@@ -503,6 +503,84 @@ extern "C" usl_status usl_redistribute_rows(usl_ctx* c, int32_t* idx, void* W, f
     c->lf[0].built_for = c->lf[1].built_for = nullptr;
     c->slot_order_for = nullptr;
     return usl_launch_redistribute_rows(c, idx, W, m1, m2, per_row, seed, epoch);
+}
+
+// ---- around the layer
+
+extern "C" usl_status usl_layer_norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean,
+                                     float* rstd, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(h); NEED(x);
+    if (!(eps > 0.f) || isinf(eps)) USL_FAIL(c, USL_EINVAL, "eps must be finite and > 0");
+    USL_TRY(check_batch(c, b));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_norm(c, h, gamma, beta, eps, x, mean, rstd, b);
+}
+
+extern "C" usl_status usl_layer_norm_backward(usl_ctx* c, const float* grad_x, const void* h, const float* gamma, const float* mean,
+                                              const float* rstd, float* grad_h, float* grad_gamma, float* grad_beta, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(grad_x); NEED(h); NEED(mean); NEED(rstd); NEED(grad_h);
+    if ((const void*)grad_h == (const void*)grad_x || (const void*)grad_h == h) USL_FAIL(c, USL_EINVAL, "grad_h is an input");
+    USL_TRY(check_batch(c, b));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_norm_grad(c, grad_x, h, gamma, mean, rstd, grad_h, grad_gamma, grad_beta, b);
+}
+
+extern "C" usl_status usl_quantize_mx4(usl_ctx* c, const void* W, uint32_t* codes, uint8_t* scales) {
+    if (!c) return USL_EINVAL;
+    NEED(W); NEED(codes); NEED(scales);
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_mx4_quantize(c, W, codes, scales);
+}
+
+extern "C" usl_status usl_dequantize_mx4(usl_ctx* c, const uint32_t* codes, const uint8_t* scales, void* W) {
+    if (!c) return USL_EINVAL;
+    NEED(codes); NEED(scales); NEED(W);
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_mx4_dequantize(c, codes, scales, W);
+}
+
+extern "C" usl_status usl_forward_mx4(usl_ctx* c, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales,
+                                      float* out, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(x); NEED(idx); NEED(codes); NEED(scales); NEED(out);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_forward_mx4(c, x, idx, codes, scales, out, b);
+}
+
+static usl_status check_adjustments(usl_ctx* c, const usl_adjustments* adj, int32_t b) {
+    NEED(adj);
+    if (!(adj->repeat > 0.f) || isinf(adj->repeat)) USL_FAIL(c, USL_EINVAL, "repeat must be finite and > 0");
+    if (!(adj->presence - adj->presence == 0.f) || !(adj->frequency - adj->frequency == 0.f))
+        USL_FAIL(c, USL_EINVAL, "presence, frequency must be finite");
+    if (!adj->shown_off != !adj->shown_lab) USL_FAIL(c, USL_EINVAL, "shown_off and shown_lab go together");
+    if (adj->allowed && adj->allowed_rows != 1 && adj->allowed_rows < b)
+        USL_FAIL(c, USL_EINVAL, "%d masks for %d instances", adj->allowed_rows, b);
+    return USL_OK;
+}
+
+extern "C" usl_status usl_adjust_scores(usl_ctx* c, const float* out, const usl_adjustments* adj, float* adjusted, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(out); NEED(adjusted);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_adjustments(c, adj, b));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_adjust(c, out, adj, adjusted, b);
+}
+
+extern "C" usl_status usl_topk_adjusted(usl_ctx* c, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk, int32_t* top_lab,
+                                        float* top_val) {
+    if (!c) return USL_EINVAL;
+    NEED(out); NEED(top_lab); NEED(top_val);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_adjustments(c, adj, b));
+    if (kk < 1) USL_FAIL(c, USL_EINVAL, "kk = %d, must be at least 1", kk);
+    if (kk > c->m || kk > usl_topk_max())
+        USL_FAIL(c, USL_ESHAPE, "kk = %d, this build takes at most min(m, %d)", kk, usl_topk_max());
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_topk_adjusted(c, out, adj, b, kk, top_lab, top_val);
 }
 
 extern "C" usl_status usl_check(usl_ctx* c) {

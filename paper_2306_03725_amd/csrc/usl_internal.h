@@ -66,6 +66,7 @@ struct usl_ctx {
     uint64_t* topk_cand;      size_t topk_cand_cap;  // [b][segments][kk] packed (score, label) keys
     uint32_t* topk_done;           // behind them: the count of a prediction's forward (k_count.h; 0 between calls)
     bool topk_done_clear;          // it has been cleared
+    float* norm_part;         size_t norm_part_cap;  // [parts of the batch][2][d] sums of the layer norm's weight and bias gradients
     float* gw_part;           size_t gw_part_cap;   // [groups][m*k] partial weight gradients of a split batch
     int gw_parts_most;             // groups that it has room for (0: not known yet)
     float* gxT;               size_t gxT_cap;  // [tiles][d][32] input gradient in the same layout
@@ -285,6 +286,16 @@ usl_status usl_launch_topk_merge(usl_ctx* ctx, int nseg, int32_t b, int32_t kk, 
 // usl_predict of one instance: the best labels from the forward kernel's workgroups (out: scratch, not to be read afterwards).  *done = false: not such a call.
 usl_status usl_launch_predict_few(usl_ctx* ctx, const void* x, const int32_t* idx, const void* W, float* out, int32_t b, int32_t kk,
                                   int32_t* top_lab, float* top_val, bool* done);
+// The operators around the layer (k_norm.hip, k_mx4.hip, k_adjust.hip).
+usl_status usl_launch_norm(usl_ctx* ctx, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b);
+usl_status usl_launch_norm_grad(usl_ctx* ctx, const float* grad_x, const void* h, const float* gamma, const float* mean, const float* rstd, float* grad_h,
+                                float* grad_gamma, float* grad_beta, int32_t b);
+usl_status usl_launch_mx4_quantize(usl_ctx* ctx, const void* W, uint32_t* codes, uint8_t* scales);
+usl_status usl_launch_mx4_dequantize(usl_ctx* ctx, const uint32_t* codes, const uint8_t* scales, void* W);
+usl_status usl_launch_forward_mx4(usl_ctx* ctx, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b);
+usl_status usl_launch_adjust(usl_ctx* ctx, const float* out, const usl_adjustments* adj, float* adjusted, int32_t b);
+usl_status usl_launch_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk, int32_t* top_lab, float* top_val);
+size_t usl_adjusted_segments(const usl_ctx* ctx);   // sets of candidates that usl_launch_topk_adjusted leaves at most
 static inline int usl_forward_few_blocks(const usl_ctx* c) { return c->num_cu * 2; }   // workgroups of its forward at most
 // dst_idx[q][:] = idx[rows[q]][:] and (if W) dst_W[q][:] = W[rows[q]][:], q < n; row ids are clamped into [0, m)
 usl_status usl_launch_gather_rows(usl_ctx* ctx, const int32_t* idx, const void* W, const int32_t* rows,

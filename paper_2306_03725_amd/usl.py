@@ -21,7 +21,9 @@ SYMBOLS = ["usl_bce_loss_grad_noalloc", "usl_check", "usl_create", "usl_destroy"
            "usl_topk", "usl_precision_hits", "usl_train_step", "usl_redistribute_rows", "usl_predict",
            "usl_forward_rows", "usl_backward_weight_rows", "usl_backward_input_rows",
            "usl_backward_weight", "usl_backward_input", "usl_backward", "usl_adam_step", "usl_redistribute",
-           "usl_validate_indices", "usl_philox_words"]
+           "usl_validate_indices", "usl_philox_words",
+           "usl_layer_norm", "usl_layer_norm_backward", "usl_quantize_mx4", "usl_dequantize_mx4", "usl_forward_mx4",
+           "usl_adjust_scores", "usl_topk_adjusted"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError("libusl.so is not built: run `python -m paper_2306_03725_amd.build` "
@@ -31,6 +33,13 @@ _lib = ctypes.CDLL(LIB_PATH)
 _vp, _i32, _i64, _u32, _u64, _f32, _f64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                            ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
                                            ctypes.c_double)
+
+
+class _Adjustments(ctypes.Structure):   # usl_adjustments
+    _fields_ = [("bias", _vp), ("allowed", _vp), ("allowed_rows", _i32), ("shown_off", _vp), ("shown_lab", _vp),
+                ("repeat", _f32), ("presence", _f32), ("frequency", _f32)]
+
+
 _sig = {
     "usl_create": [ctypes.POINTER(_vp), _i64, _i32, _i32, _i32, ctypes.c_int, _vp],
     "usl_destroy": [_vp],
@@ -58,6 +67,13 @@ _sig = {
     "usl_redistribute_rows": [_vp, _vp, _vp, _vp, _vp, _i32, _u64, _u64],
     "usl_validate_indices": [_vp, _vp, ctypes.POINTER(_i64)],
     "usl_philox_words": [_vp, _vp, _u32, _u32, _vp, _i64],
+    "usl_layer_norm": [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _i32],
+    "usl_layer_norm_backward": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32],
+    "usl_quantize_mx4": [_vp, _vp, _vp, _vp],
+    "usl_dequantize_mx4": [_vp, _vp, _vp, _vp],
+    "usl_forward_mx4": [_vp, _vp, _vp, _vp, _vp, _vp, _i32],
+    "usl_adjust_scores": [_vp, _vp, ctypes.POINTER(_Adjustments), _vp, _i32],
+    "usl_topk_adjusted": [_vp, _vp, ctypes.POINTER(_Adjustments), _i32, _i32, _vp, _vp],
 }
 for _name, _args in _sig.items():
     _f = getattr(_lib, _name)
@@ -88,6 +104,19 @@ def _ptr(t):
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return t.data_ptr()
+
+
+class Adjustments:
+    """usl_adjustments: what happens to scores before they are ranked.  bias [m] float32; allowed [1 or b][ceil(m/32)] int32 words, a
+    bit a label; shown_off [b+1] int64 and shown_lab int32, the labels each instance has been shown.  All are optional, and kept."""
+
+    def __init__(self, bias=None, allowed=None, shown_off=None, shown_lab=None, repeat=1.0, presence=0.0, frequency=0.0, allowed_rows=None):
+        self.tensors = (bias, allowed, shown_off, shown_lab)
+        if allowed_rows is None:   # of a raw address: one mask for all, unless said otherwise
+            allowed_rows = 1 if allowed is None or isinstance(allowed, int) or allowed.dim() < 2 else allowed.shape[0]
+        if shown_lab is not None and not isinstance(shown_lab, int) and shown_lab.numel() == 0:
+            shown_off = shown_lab = None   # (a tensor without elements has no address)
+        self._a = _Adjustments(_ptr(bias), _ptr(allowed), allowed_rows, _ptr(shown_off), _ptr(shown_lab), repeat, presence, frequency)
 
 
 class Layer:
@@ -217,3 +246,26 @@ class Layer:
 
     def philox_words(self, ctr, key0, key1, out, n):
         self._ck(_lib.usl_philox_words(self._h, _ptr(ctr), key0, key1, _ptr(out), n))
+
+    def layer_norm(self, h, gamma, beta, eps, x, mean, rstd, b):
+        self._ck(_lib.usl_layer_norm(self._h, _ptr(h), _ptr(gamma), _ptr(beta), eps, _ptr(x), _ptr(mean), _ptr(rstd), b))
+
+    def layer_norm_backward(self, grad_x, h, gamma, mean, rstd, grad_h, grad_gamma, grad_beta, b):
+        self._ck(_lib.usl_layer_norm_backward(self._h, _ptr(grad_x), _ptr(h), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(grad_h),
+                                              _ptr(grad_gamma), _ptr(grad_beta), b))
+
+    def quantize_mx4(self, W, codes, scales):
+        self._ck(_lib.usl_quantize_mx4(self._h, _ptr(W), _ptr(codes), _ptr(scales)))
+
+    def dequantize_mx4(self, codes, scales, W):
+        self._ck(_lib.usl_dequantize_mx4(self._h, _ptr(codes), _ptr(scales), _ptr(W)))
+
+    def forward_mx4(self, x, idx, codes, scales, out, b):
+        self._same_idx(idx)
+        self._ck(_lib.usl_forward_mx4(self._h, _ptr(x), _ptr(idx), _ptr(codes), _ptr(scales), _ptr(out), b))
+
+    def adjust_scores(self, out, adjustments, adjusted, b):
+        self._ck(_lib.usl_adjust_scores(self._h, _ptr(out), ctypes.byref(adjustments._a), _ptr(adjusted), b))
+
+    def topk_adjusted(self, out, adjustments, b, kk, top_lab, top_val):
+        self._ck(_lib.usl_topk_adjusted(self._h, _ptr(out), ctypes.byref(adjustments._a), b, kk, _ptr(top_lab), _ptr(top_val)))
