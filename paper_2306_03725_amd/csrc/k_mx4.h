@@ -19,3 +19,7 @@ __device__ __forceinline__ float mx4_code(uint32_t code) {
     const uint32_t em = code & 7u, bits = em < 2u ? (em ? 0x3F000000u : 0u) : ((em >> 1) + 126u) << 23 | (em & 1u) << 22;
     return __uint_as_float(bits | (code & 8u) << 28);
 }
+// slot t of label j
+__device__ __forceinline__ float mx4_value(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t j, int t, int k) {
+    return mx4_code(codes[j * mx4_words(k) + t / 8] >> (4 * (t % 8))) * mx4_scale(scales[j * mx4_blocks(k) + t / MX4_BLOCK]);
+}

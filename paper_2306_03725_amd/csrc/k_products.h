@@ -7,8 +7,8 @@
 namespace usl_products {
 
 // FORWARD_CACHED: the scores go through the caches where FORWARD's go past them (K = 24 and four instances a read; others: FORWARD's kernel); FORWARD_LOSS: the scores become
-// the gradient of the loss; FORWARD_MARKS: of the squared hinge, and its nonzeros are marked
-enum ProductKind { FORWARD, FORWARD_CACHED, FORWARD_LOSS, FORWARD_MARKS, WEIGHT_GRADIENT };
+// the gradient of the loss; FORWARD_MARKS: of the squared hinge, and its nonzeros are marked; FORWARD_MX4: the scores from values in 4 bits
+enum ProductKind { FORWARD, FORWARD_CACHED, FORWARD_LOSS, FORWARD_MARKS, FORWARD_MX4, WEIGHT_GRADIENT };
 
 struct ProductKernel {
     const void* fn;        // nullptr: no such kernel

@@ -205,11 +205,13 @@ __device__ __forceinline__ float moved(float v) { return __int_as_float(__builti
 // it takes 10 more registers, with which a compute unit holds one workgroup of 1024 in the place of two where k is no multiple of 4.  Where it is used:
 // best_from_forward.  (Several instances one after the other took longer than a kernel over the scores: m = 31k, d = 1k, k = 32, b = 4 16.2 and 26.6.)
 constexpr int FEW_HELD = 4;   // turns whose scores, or candidates, a lane keeps in registers
-template <int LPL, typename TS, int Q, bool VEC, int AHEAD, bool BEST>
+// MX4: W are the codes of values in 4 bits (k_mx4.h).  Two lanes share a word of eight codes; a lane's four slots lie in one block, so its sum of
+// codes times activations is scaled once.
+template <int LPL, typename TS, int Q, bool VEC, int AHEAD, bool BEST, bool MX4 = false>
 __global__ void __launch_bounds__(1024)
 k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS* __restrict__ W, float* __restrict__ out,
               int64_t m, int k, int b, int row_bytes, int rounds, int kk, uint64_t* __restrict__ cand, uint32_t* __restrict__ done,
-              int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
+              int32_t* __restrict__ top_lab, float* __restrict__ top_val, const uint8_t* __restrict__ scales) {
     typedef typename Unit<TS, Q>::T U;
     extern __shared__ __align__(16) unsigned char lds_raw[];
     const uint32_t lds0 = lds_base(lds_raw);
@@ -227,7 +229,20 @@ k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, cons
     auto fetch = [&](int64_t j0, int r, Piece& p) {
         const int64_t j = j0 + r * (64 / LPL) + lane / LPL;
         const bool in = j < m && t < k;
-        if (VEC) {
+        if constexpr (MX4) {
+            uint4 c = make_uint4(nowhere, nowhere, nowhere, nowhere);
+            if (VEC) {
+                if (in) c = *reinterpret_cast<const uint4*>(idx + j * k + t);
+            } else if (in) {
+                c.x = (uint32_t)idx[j * k + t];
+                if (t + 1 < k) c.y = (uint32_t)idx[j * k + t + 1];
+                if (t + 2 < k) c.z = (uint32_t)idx[j * k + t + 2];
+                if (t + 3 < k) c.w = (uint32_t)idx[j * k + t + 3];
+            }
+            p.c[0] = c.x; p.c[1] = c.y; p.c[2] = c.z; p.c[3] = c.w;
+            p.w[0] = in ? reinterpret_cast<const uint32_t*>(W)[j * mx4_words(k) + (t >> 3)] : 0u;
+            p.w[1] = in ? scales[j * mx4_blocks(k) + t / MX4_BLOCK] : 127u;
+        } else if (VEC) {
             uint4 c = make_uint4(nowhere, nowhere, nowhere, nowhere);
             if (in) c = *reinterpret_cast<const uint4*>(idx + j * k + t);
             p.c[0] = c.x; p.c[1] = c.y; p.c[2] = c.z; p.c[3] = c.w;
@@ -256,7 +271,39 @@ k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, cons
         U v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = activation(p.c[q]);
-        if constexpr (sizeof(TS) == 4) {
+        if constexpr (MX4) {
+            const uint32_t half = p.w[0] >> (16 * (sub & 1));
+            const float scale = mx4_scale(p.w[1]);
+#pragma unroll
+            for (int q = 0; q < 4; q += 2) {
+                if constexpr (sizeof(TS) == 4) {
+                    const f32x2 w = q ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 1) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 0);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if constexpr (Q == 1) acc[0] = fmaf(w[u], v[q + u], acc[0]);
+                        else {
+#pragma unroll
+                            for (int i = 0; i < Q; ++i) acc[i] = fmaf(w[u], v[q + u][i], acc[i]);
+                        }
+                    }
+                } else {
+                    const uint32_t w = __builtin_bit_cast(uint32_t, q ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 1)
+                                                                     : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 0));
+                    if constexpr (Q == 1) acc[0] = dot2((uint32_t)v[q] | ((uint32_t)v[q + 1] << 16), w, acc[0]);
+                    else if constexpr (Q == 2) {
+                        acc[0] = dot2(join_lo(v[q], v[q + 1]), w, acc[0]);
+                        acc[1] = dot2(join_hi(v[q], v[q + 1]), w, acc[1]);
+                    } else {
+                        acc[0] = dot2(join_lo(v[q].x, v[q + 1].x), w, acc[0]);
+                        acc[1] = dot2(join_hi(v[q].x, v[q + 1].x), w, acc[1]);
+                        acc[2] = dot2(join_lo(v[q].y, v[q + 1].y), w, acc[2]);
+                        acc[3] = dot2(join_hi(v[q].y, v[q + 1].y), w, acc[3]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < Q; ++i) acc[i] *= scale;
+        } else if constexpr (sizeof(TS) == 4) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float w = __uint_as_float(p.w[q]);
@@ -403,11 +450,11 @@ k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, cons
 }
 
 // out[i][:] once more, slot by slot, for the instances whose activation 0 is not finite (see pads_with_column_0): nearly
-// always none, and a block that finds none leaves.  A lane per label.
+// always none, and a block that finds none leaves.  A lane per label.  scales: of values in 4 bits, whose codes W are; else nullptr.
 template <typename TS>
 __global__ void __launch_bounds__(256)
 k_forward_again(const TS* __restrict__ x, const int32_t* __restrict__ idx, const TS* __restrict__ W, float* __restrict__ out, int64_t m, int d,
-                int k, int b) {
+                int k, int b, const uint8_t* __restrict__ scales) {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int lane = threadIdx.x & 63;
     for (int i0 = 0; i0 < b; i0 += 64) {
@@ -417,7 +464,10 @@ k_forward_again(const TS* __restrict__ x, const int32_t* __restrict__ idx, const
             const int i = i0 + __ffsll((unsigned long long)todo) - 1;
             if (j >= m) continue;
             float acc = 0.f;
-            for (int t = 0; t < k; ++t) acc = fmaf(usl_load_f32<TS>(W, (size_t)j * k + t), usl_load_f32<TS>(x, (size_t)i * d + idx[j * k + t]), acc);
+            for (int t = 0; t < k; ++t) {
+                const float w = scales ? mx4_value(reinterpret_cast<const uint32_t*>(W), scales, j, t, k) : usl_load_f32<TS>(W, (size_t)j * k + t);
+                acc = fmaf(w, usl_load_f32<TS>(x, (size_t)i * d + idx[j * k + t]), acc);
+            }
             out[(size_t)i * m + j] = acc;
         }
     }
@@ -828,8 +878,9 @@ bool last_one_merges(const usl_ctx* c, const FewShape& f, int kk) {
 }
 
 // One group of instances: the streaming kernel.  kk > 0, one instance: its best labels; out is scratch then, written only by wavefronts of more than FEW_HELD turns.
+// mx4: the scales of values in 4 bits, whose codes W are.
 usl_status run_forward_few(usl_ctx* c, const Layout& L, const void* x, const int32_t* idx, const void* W, float* out, int b, int kk = 0, int32_t* top_lab = nullptr,
-                           float* top_val = nullptr) {
+                           float* top_val = nullptr, const uint8_t* mx4 = nullptr) {
     const void* xi = nullptr;
     USL_TRY(activations(c, L, x, b, &xi));
     const FewShape f = few_shape(c, L, kk);
@@ -844,14 +895,19 @@ usl_status run_forward_few(usl_ctx* c, const Layout& L, const void* x, const int
         cand = c->topk_cand;
         merge = c->topk_done_clear && last_one_merges(c, f, kk);
     }
-#define USL_FEW_B(LPL, TS, Q, VEC, AHEAD, BEST)                                                                    \
+#define USL_FEW_B(LPL, TS, Q, VEC, AHEAD, BEST, MX4)                                                               \
     do {                                                                                                                \
-        USL_TRY(allow_lds(c, k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST>, lds));                                    \
-        hipLaunchKernelGGL((k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST>), dim3(grid), dim3((unsigned)nw * 64), lds, c->stream,        \
+        USL_TRY(allow_lds(c, k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST, MX4>, lds));                               \
+        hipLaunchKernelGGL((k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST, MX4>), dim3(grid), dim3((unsigned)nw * 64), lds, c->stream,   \
                            (const char*)xi, idx, (const TS*)W, out, c->m, c->k, b, L.row_bytes, rounds, kk, cand,      \
-                           c->topk_done, merge ? top_lab : nullptr, top_val);                                                          \
+                           c->topk_done, merge ? top_lab : nullptr, top_val, mx4);                                                     \
     } while (0)
-#define USL_FEW_A(LPL, TS, Q, VEC, AHEAD) do { if (Q == 1 && kk > 0) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, (Q == 1)); else USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false); } while (0)
+#define USL_FEW_A(LPL, TS, Q, VEC, AHEAD)                                                                          \
+    do {                                                                                                                \
+        if (mx4) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false, true);                                                       \
+        else if (Q == 1 && kk > 0) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, (Q == 1), false);                                 \
+        else USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false, false);                                                          \
+    } while (0)
 #define USL_FEW(LPL, TS, Q, VEC)                                                                                    \
     do {                                                                                                                \
         if (Q == 1 && LPL >= 4 && rounds >= 4) USL_FEW_A(LPL, TS, Q, VEC, (Q == 1 && LPL >= 4 ? 4 : 2));            \
@@ -901,8 +957,8 @@ bool scores_through_caches(const usl_ctx* c, const Layout& L, const float* out, 
 // the forward kernel over the whole batch, with or without the loss (then `before` says what the targets are; their bits are set
 // here and taken back by the kernel that ends the step)
 usl_status run_forward(usl_ctx* c, const Layout& L, const void* x, const int32_t* idx, const void* W, float* out, int32_t b, LossArgs loss,
-                       size_t* blocks, Before before = Before{}) {
-    const Launch p = choose(c, L, b, loss.nonzeros ? FORWARD_MARKS : loss.kind >= 0 ? FORWARD_LOSS : scores_through_caches(c, L, out, b) ? FORWARD_CACHED : FORWARD);
+                       size_t* blocks, Before before = Before{}, const uint8_t* mx4 = nullptr) {
+    const Launch p = choose(c, L, b, mx4 ? FORWARD_MX4 : loss.nonzeros ? FORWARD_MARKS : loss.kind >= 0 ? FORWARD_LOSS : scores_through_caches(c, L, out, b) ? FORWARD_CACHED : FORWARD);
     const uint8_t* perm = nullptr;
     const void* xi = nullptr;
     USL_TRY(slot_order(c, idx, &perm));
@@ -926,7 +982,7 @@ usl_status run_forward(usl_ctx* c, const Layout& L, const void* x, const int32_t
         loss.partials = c->bce_partials;
     }
     Tail tail = p.tail;
-    void* args[] = {&xi, &idx, &W, &out, &m, &k, &bb, &tg, &perm, &loss, &tail};
+    void* args[] = {&xi, &idx, &W, &out, &m, &k, &bb, &tg, &perm, &loss, &tail, &mx4};
     return launch(c, p, args, "forward");
 }
 
@@ -934,19 +990,29 @@ bool streams(const usl_ctx* c, const Layout& L, int b) { return b <= L.Q && !L.h
 
 }  // namespace
 
-usl_status usl_launch_forward(usl_ctx* c, const void* x, const int32_t* idx, const void* W, float* out, int32_t b) {
-    if (!fast_path_ok(c, idx, W))
-        return c->storage == USL_F32 ? run_forward_generic<float>(c, x, idx, W, out, b) : run_forward_generic<uint16_t>(c, x, idx, W, out, b);
+// mx4: the scales of values in 4 bits, whose codes W are
+static usl_status forward_by_gathers(usl_ctx* c, const void* x, const int32_t* idx, const void* W, const uint8_t* mx4, float* out, int32_t b) {
     const Layout L = layout_of(c, b, x);
-    if (streams(c, L, b)) return run_forward_few(c, L, x, idx, W, out, b);
-    USL_TRY(run_forward(c, L, x, idx, W, out, b, LossArgs{-1, 0.f, nullptr, nullptr, nullptr, 0, nullptr}, nullptr));
+    if (streams(c, L, b)) return run_forward_few(c, L, x, idx, W, out, b, 0, nullptr, nullptr, mx4);
+    USL_TRY(run_forward(c, L, x, idx, W, out, b, LossArgs{-1, 0.f, nullptr, nullptr, nullptr, 0, nullptr}, nullptr, Before{}, mx4));
     if (!pads_with_column_0(c, L)) return USL_OK;
     const dim3 grid((unsigned)((c->m + 255) / 256));
     if (c->storage == USL_F32)
-        hipLaunchKernelGGL(k_forward_again<float>, grid, dim3(256), 0, c->stream, (const float*)x, idx, (const float*)W, out, c->m, c->d, c->k, b);
+        hipLaunchKernelGGL(k_forward_again<float>, grid, dim3(256), 0, c->stream, (const float*)x, idx, (const float*)W, out, c->m, c->d, c->k, b, mx4);
     else
-        hipLaunchKernelGGL(k_forward_again<uint16_t>, grid, dim3(256), 0, c->stream, (const uint16_t*)x, idx, (const uint16_t*)W, out, c->m, c->d, c->k, b);
+        hipLaunchKernelGGL(k_forward_again<uint16_t>, grid, dim3(256), 0, c->stream, (const uint16_t*)x, idx, (const uint16_t*)W, out, c->m, c->d, c->k, b, mx4);
     return usl_check_launch(c, "forward (activations that are not finite)");
+}
+
+usl_status usl_launch_forward(usl_ctx* c, const void* x, const int32_t* idx, const void* W, float* out, int32_t b) {
+    if (!fast_path_ok(c, idx, W))
+        return c->storage == USL_F32 ? run_forward_generic<float>(c, x, idx, W, out, b) : run_forward_generic<uint16_t>(c, x, idx, W, out, b);
+    return forward_by_gathers(c, x, idx, W, nullptr, out, b);
+}
+
+usl_status usl_launch_forward_mx4(usl_ctx* c, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b) {
+    if (!fast_path_ok(c, idx, nullptr)) return usl_launch_forward_mx4_any(c, x, idx, codes, scales, out, b);
+    return forward_by_gathers(c, x, idx, codes, scales, out, b);
 }
 
 usl_status usl_launch_predict_few(usl_ctx* c, const void* x, const int32_t* idx, const void* W, float* out, int32_t b, int32_t kk,

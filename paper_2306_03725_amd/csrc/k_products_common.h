@@ -20,7 +20,7 @@
 #pragma once
 #include <type_traits>
 
-#include "usl_internal.h"
+#include "k_mx4.h"
 
 namespace usl_products {
 
@@ -428,6 +428,49 @@ __device__ __forceinline__ void unpack_w(const RawRows<uint16_t, K>& raw, int k,
     }
     wave_sync();
 }
+// Values in 4 bits (k_mx4.h): the words and scales of this lane's label, and its weights in the label's slot order, float32 or pairs of
+// bfloat16 (both hold them exactly).  A lane reads its own row only: its words go through its wavefront's piece of LDS to be picked by slot.
+template <int K>
+struct Mx4Row {
+    uint32_t code[K / 8];
+    float scale[(K + 31) / 32];
+    __device__ __forceinline__ void load(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t j, bool valid, int k) {
+        const int nw = mx4_words(k), nb = mx4_blocks(k);
+#pragma unroll
+        for (int q = 0; q < K / 8; ++q) code[q] = valid && q < nw ? codes[j * nw + q] : 0u;
+#pragma unroll
+        for (int q = 0; q < (K + 31) / 32; ++q) scale[q] = mx4_scale(valid && q < nb ? scales[j * nb + q] : 127u);
+    }
+    __device__ __forceinline__ float at(const uint32_t* mine, int slot, int k) const {
+        const float s = K > 32 && slot >= 32 ? scale[K > 32 ? 1 : 0] : scale[0];
+        return slot < k ? mx4_code(mine[slot >> 3] >> (4 * (slot & 7))) * s : 0.f;   // (a padding slot's weight is 0 whatever the scale)
+    }
+    __device__ __forceinline__ uint32_t* put(uint32_t* lds) const {
+        uint32_t* mine = lds + (threadIdx.x >> 6) * 64 * halves_stride<K>() + (threadIdx.x & 63) * (K / 8 + 1);
+#pragma unroll
+        for (int q = 0; q < K / 8; ++q) mine[q] = code[q];
+        wave_sync();
+        return mine;
+    }
+    __device__ __forceinline__ void unpack(uint32_t* lds, const SlotOrder<K>& so, int k, float (&w)[K]) const {
+        const uint32_t* mine = put(lds);
+#pragma unroll
+        for (int s = 0; s < K; ++s) {
+            w[s] = at(mine, so.at(s), k);
+            if ((s & 7) == 7) __builtin_amdgcn_sched_barrier(0);
+        }
+        wave_sync();
+    }
+    __device__ __forceinline__ void unpack(uint32_t* lds, const SlotOrder<K>& so, int k, uint32_t (&wp)[K / 2]) const {
+        const uint32_t* mine = put(lds);
+#pragma unroll
+        for (int q = 0; q < K / 2; ++q) {
+            wp[q] = __float_as_uint(at(mine, so.at(2 * q), k)) >> 16 | (__float_as_uint(at(mine, so.at(2 * q + 1), k)) & 0xFFFF0000u);
+            if ((q & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        wave_sync();
+    }
+};
 // The reverse: acc[s] of every lane becomes row row0 + threadIdx.x of dst[m][k].  All threads of the workgroup call it.
 template <int K, int NT>
 __device__ __forceinline__ void store_rows(const float (&acc)[K], float* __restrict__ dst, int64_t row0, int64_t m, int k,
@@ -703,10 +746,11 @@ struct LossArgs {
 // LOSS: 0 the scores, 1 either loss, 2 the squared hinge with its nonzeros marked, one bit per score, where few of them are expected: the
 // pass over g that listed them took 105 us at m = 500k, b = 256, and clearing the weight gradient, which goes out here while the chip waits
 // for LDS anyway, 11.  (Instances of their own: with a test at run time the step of the binary cross-entropy there took 1 % longer.)
-template <int K, int LPT, int NT, typename TS, int Q, bool HALVES, int LOSS, bool EVEN, bool CACHED>
+// MX4: W are the codes of values in 4 bits, and scales their blocks' scales; the weights are decoded once, on their way into the registers.
+template <int K, int LPT, int NT, typename TS, int Q, bool HALVES, int LOSS, bool EVEN, bool CACHED, bool MX4 = false>
 __global__ void __launch_bounds__(NT)
 k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS* __restrict__ W, float* __restrict__ out,
-          int64_t m, int k, int b, Geom tg, const uint8_t* __restrict__ perm, LossArgs loss, Tail tail) {
+          int64_t m, int k, int b, Geom tg, const uint8_t* __restrict__ perm, LossArgs loss, Tail tail, const uint8_t* __restrict__ scales) {
     extern __shared__ __align__(16) unsigned char lds_raw[];
     const uint32_t lds0 = lds_base(lds_raw);
     const Turn turn(tg, tail);
@@ -726,7 +770,21 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
 #pragma unroll
     for (int l = 0; l < LPT; ++l) {
         const int64_t row0 = j0 + (int64_t)l * NT;
-        if constexpr (raw_rows<TS, K, NT>()) {
+        if constexpr (MX4) {
+            Mx4Row<K> row;
+            row.load(reinterpret_cast<const uint32_t*>(W), scales, row0 + threadIdx.x, row0 + threadIdx.x < end, k);
+            SlotOrder<K> so;
+            if constexpr (raw_rows<TS, K, NT>()) {
+                RawRows<TS, K> raw;
+                raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
+                unpack_idx<K, TS>(raw, k, reinterpret_cast<uint32_t*>(lds_raw), pk[l]);
+                so = raw.so;
+            } else {
+                so.load(perm, row0 + threadIdx.x, row0 + threadIdx.x < end);
+                fetch_idx<K>(idx, row0, end, k, (uint32_t)tg.zero_col, reinterpret_cast<uint32_t*>(lds_raw), so, pk[l]);
+            }
+            row.unpack(reinterpret_cast<uint32_t*>(lds_raw), so, k, w[l].v);
+        } else if constexpr (raw_rows<TS, K, NT>()) {
             RawRows<TS, K> raw;
             raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
             raw.load_w(W, row0, end, k);

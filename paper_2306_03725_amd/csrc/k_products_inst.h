@@ -25,6 +25,7 @@ ProductKernel pick(ProductKind kind, int shape) {
 #define USL_FORWARD_KIND(LPT, NT, EVEN)                                                                        \
     (kind == FORWARD_MARKS    ? (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 2, EVEN, false>               \
      : kind == FORWARD_LOSS   ? (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 1, EVEN, false>               \
+     : kind == FORWARD_MX4    ? (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 0, EVEN, (K <= 16), true>      \
      : kind == FORWARD_CACHED ? (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 0, EVEN, (K <= 16 || (K == 24 && Q == 4))> \
                               : (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 0, EVEN, (K <= 16)>)
 #define USL_FORWARD(LPT, NT) ProductKernel{USL_FORWARD_KIND(LPT, NT, false), USL_FORWARD_KIND(LPT, NT, true), K, LPT, NT, transpose_bytes<K, NT>()}

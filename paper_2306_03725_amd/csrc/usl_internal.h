@@ -293,6 +293,7 @@ usl_status usl_launch_norm_grad(usl_ctx* ctx, const float* grad_x, const void* h
 usl_status usl_launch_mx4_quantize(usl_ctx* ctx, const void* W, uint32_t* codes, uint8_t* scales);
 usl_status usl_launch_mx4_dequantize(usl_ctx* ctx, const uint32_t* codes, const uint8_t* scales, void* W);
 usl_status usl_launch_forward_mx4(usl_ctx* ctx, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b);
+usl_status usl_launch_forward_mx4_any(usl_ctx* ctx, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b);   // any k, any d
 usl_status usl_launch_adjust(usl_ctx* ctx, const float* out, const usl_adjustments* adj, float* adjusted, int32_t b);
 usl_status usl_launch_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk, int32_t* top_lab, float* top_val);
 size_t usl_adjusted_segments(const usl_ctx* ctx);   // sets of candidates that usl_launch_topk_adjusted leaves at most
