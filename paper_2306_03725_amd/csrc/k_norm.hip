@@ -6,6 +6,92 @@
 
 namespace {
 
+template <typename TS> __device__ __forceinline__ TS stored(float v);
+template <> __device__ __forceinline__ float stored<float>(float v) { return v; }
+template <> __device__ __forceinline__ uint16_t stored<uint16_t>(float v) { return usl_f32_to_bf16(v); }   // the one rounding of a result
+
+// ---- 16 bytes of a row at a time: 4 values of float32, 8 of bfloat16; rows begin at any value --------------------
+typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
+template <typename TS> constexpr int VEC = 16 / (int)sizeof(TS);
+
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[4]) {
+    const f32x4 q = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = q[e];
+}
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[8]) {
+    const f32x4 q = *reinterpret_cast<const f32x4*>(p), r = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = q[e]; v[4 + e] = r[e]; }
+}
+__device__ __forceinline__ void load_vec(const uint16_t* p, float (&v)[8]) {
+    const u16x8 q = *reinterpret_cast<const u16x8*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = usl_bf16_to_f32(q[e]);
+}
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[4]) {
+    const f32x4 q = {v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4*>(p) = q;
+}
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[8]) {
+    const f32x4 q = {v[0], v[1], v[2], v[3]}, r = {v[4], v[5], v[6], v[7]};
+    *reinterpret_cast<f32x4*>(p) = q;
+    *reinterpret_cast<f32x4*>(p + 4) = r;
+}
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&v)[8]) {
+    u16x8 q;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = usl_f32_to_bf16(v[e]);
+    *reinterpret_cast<u16x8*>(p) = q;
+}
+
+// How LANES lanes divide a row of d values: the whole groups of V values are dealt to the lanes in turn, the values behind them (fewer than V) go one to a lane.
+// (With the last group taken value by value every load and store has V branches, and the kernels spill.)
+template <int LANES, int V>
+struct RowShare {
+    int lane, whole, rest;   // values in whole groups, values behind them
+    __device__ __forceinline__ RowShare(int lane_, int d) : lane(lane_), whole(d / V * V), rest(d % V) {}
+    __device__ __forceinline__ int at(int g) const { return (g * LANES + lane) * V; }
+    __device__ __forceinline__ bool has(int g) const { return at(g) < whole; }
+    __device__ __forceinline__ bool has_rest() const { return lane < rest; }
+    template <typename T, int G>
+    __device__ __forceinline__ void load(const T* __restrict__ row, float (&v)[G][V], float& last, float fill) const {
+#pragma unroll
+        for (int g = 0; g < G; ++g) load_group(row, g, v[g], fill);
+        last = has_rest() ? usl_to_f32(row[whole + lane]) : fill;
+    }
+    template <typename T>
+    __device__ __forceinline__ void load_group(const T* __restrict__ row, int g, float (&v)[V], float fill) const {
+        if (has(g)) {
+            load_vec(row + at(g), v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fill;
+        }
+    }
+};
+
+// ---- sums over lanes --------------------------------------------------------------------------------------------
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xF, true)); }
+// over 16 neighbouring lanes, in all of them (lanes that have been added up are alike: a mirror reaches the others as well)
+__device__ __forceinline__ float sum16(float v) {
+    v += moved<0xB1>(v);    // quads 1 0 3 2
+    v += moved<0x4E>(v);    // quads 2 3 0 1
+    v += moved<0x141>(v);   // 8 lanes, mirrored
+    v += moved<0x140>(v);   // 16
+    return v;
+}
+__device__ __forceinline__ float sum64(float v) {
+    v = sum16(v);
+    v += moved<0x142, 0xA>(v);   // the last lane of rows 0 and 2 into rows 1 and 3 (0 into the others), of row 1 into rows 2 and 3
+    v += moved<0x143, 0xC>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float v) { return LANES == 16 ? sum16(v) : sum64(v); }
+
 // Sum of v over the workgroup, returned to every lane.  red: one value a wavefront.
 template <int NT, typename T>
 __device__ __forceinline__ T block_sum(T v, T* red) {
@@ -19,15 +105,104 @@ __device__ __forceinline__ T block_sum(T v, T* red) {
     return s;
 }
 
-template <typename TS> __device__ __forceinline__ TS stored(float v);
-template <> __device__ __forceinline__ float stored<float>(float v) { return v; }
-template <> __device__ __forceinline__ uint16_t stored<uint16_t>(float v) { return usl_f32_to_bf16(v); }   // the one rounding of a result
+// ---- forward: a row in the registers of LANES lanes, EPL values each (and one of the values behind the groups) --
+// Read once, written once.  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
+// around the row's mean, behind one barrier:  M2 = sum_w M2_w + n_w (mean_w - mean)^2.
+template <typename TS, int LANES, int EPL>
+__global__ void __launch_bounds__((LANES < 256 ? 256 : LANES))
+k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, TS* x /* may be h */, float* __restrict__ mean_out,
+       float* __restrict__ rstd_out, int b, int d) {
+    constexpr int V = VEC<TS>, G = EPL / V, NT = LANES < 256 ? 256 : LANES, WAVES = LANES / 64;
+    constexpr bool EARLY = EPL <= 16;   // weight and bias come with the row; more registers than that are not left
+    int i = (int)blockIdx.x * (NT / LANES) + (int)threadIdx.x / LANES;
+    if (LANES >= 64) i = __builtin_amdgcn_readfirstlane(i);
+    if (i >= b) return;   // (rows of several wavefronts have a workgroup each)
+    const RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
+    float v[G][V], last, wg[EARLY ? G : 1][V], wb[EARLY ? G : 1][V];
+    mine.load(h + (size_t)i * d, v, last, 0.f);
+    if constexpr (EARLY) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) { wg[g][e] = 1.f; wb[g][e] = 0.f; }
+            if (gamma) mine.load_group(gamma, g, wg[g], 0.f);
+            if (beta) mine.load_group(beta, g, wb[g], 0.f);
+        }
+    }
+    const float last_w = gamma && mine.has_rest() ? gamma[mine.whole + mine.lane] : 1.f, last_b = beta && mine.has_rest() ? beta[mine.whole + mine.lane] : 0.f;
+    float s = last;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        float t = v[g][0];
+#pragma unroll
+        for (int e = 1; e < V; ++e) t += v[g][e];
+        s += t;
+    }
+    int n = d;   // values of this wavefront
+    if (LANES > 64) {
+        const int wave0 = __builtin_amdgcn_readfirstlane((int)threadIdx.x & ~63);
+        n = min(max(mine.rest - wave0, 0), 64);
+#pragma unroll
+        for (int g = 0; g < G; ++g) n += min(max(mine.whole - (g * LANES + wave0) * V, 0), 64 * V);
+    }
+    float mean = n ? sum_lanes<LANES>(s) / (float)n : 0.f;
+    float m2 = mine.has_rest() ? (last - mean) * (last - mean) : 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        float t = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) t = fmaf(v[g][e] - mean, v[g][e] - mean, t);
+        m2 += mine.has(g) ? t : 0.f;
+    }
+    m2 = sum_lanes<LANES>(m2);
+    if constexpr (LANES > 64) {
+        __shared__ float part[3][WAVES];
+        if ((threadIdx.x & 63) == 0) {
+            part[0][threadIdx.x >> 6] = mean;
+            part[1][threadIdx.x >> 6] = m2;
+            part[2][threadIdx.x >> 6] = (float)n;
+        }
+        __syncthreads();
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) all = fmaf(part[0][w], part[2][w], all);
+        mean = all / (float)d;
+        m2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float off = part[0][w] - mean;
+            m2 += fmaf(part[2][w] * off, off, part[1][w]);
+        }
+    }
+    const float rstd = 1.f / sqrtf(m2 / (float)d + eps);
+    if (mine.lane == 0) {
+        if (mean_out) mean_out[i] = mean;
+        if (rstd_out) rstd_out[i] = rstd;
+    }
+    TS* to = x + (size_t)i * d;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        float o[V], w[V], c[V];
+        if constexpr (EARLY) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) { w[e] = wg[g][e]; c[e] = wb[g][e]; }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) { w[e] = 1.f; c[e] = 0.f; }
+            if (gamma) mine.load_group(gamma, g, w, 0.f);
+            if (beta) mine.load_group(beta, g, c, 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf((v[g][e] - mean) * rstd, w[e], c[e]);
+        if (mine.has(g)) store_vec(to + mine.at(g), o);
+        if (!EARLY && g % 2) __builtin_amdgcn_sched_barrier(0);   // a few groups' weights at a time
+    }
+    if (mine.has_rest()) to[mine.whole + mine.lane] = stored<TS>(fmaf((last - mean) * rstd, last_w, last_b));
+}
 
-// ---- any d: a workgroup a row, which it reads once for every sum and once more to write -------------------------
-// (Sums in 64 bits: a lane may have thousands of values.)
-
+// Rows that registers do not hold: a workgroup a row, which it reads once for every sum and once more to write.  (Sums in 64 bits: a lane may
+// have thousands of values.)
 constexpr int ANY_NT = 1024;
-
 template <typename TS>
 __global__ void __launch_bounds__(ANY_NT)
 k_norm_any(const TS* h, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, TS* x /* may be h */,
@@ -53,60 +228,302 @@ k_norm_any(const TS* h, const float* __restrict__ gamma, const float* __restrict
     }
 }
 
+// ---- backward, rows of up to 16384: a row in the registers of LANES lanes, EPL values each -----------------------
+// A workgroup of 1024 lanes takes 1024 / LANES rows at a time, its share of the batch one after the other, and keeps the sums of grad_x n and grad_x
+// of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined pairwise through LDS, always in the same order,
+// and left in part[workgroup][2][d] (with one workgroup: in the gradients themselves).
+constexpr int BWD_NT = 1024;
+template <typename TS, int LANES, int EPL>
+__global__ void __launch_bounds__(BWD_NT)
+k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
+            const float* __restrict__ rstd_in, float* __restrict__ grad_h, float* __restrict__ to_gamma, float* __restrict__ to_beta, size_t stride, int b, int d) {
+    constexpr int V = VEC<TS>, G = EPL / V, ROWS = BWD_NT / LANES, WAVES = LANES / 64;
+    extern __shared__ __align__(16) float lds[];   // [ROWS / 2][2][EPL + 1][LANES]
+    __shared__ float part[2][2][BWD_NT / 64];
+    const RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
+    int group = (int)threadIdx.x / LANES;
+    if (LANES >= 64) group = __builtin_amdgcn_readfirstlane(group);
+    float sg[G][V] = {}, sb[G][V] = {}, last_sg = 0.f, last_sb = 0.f;
+    int turn = 0;
+    for (int i0 = (int)blockIdx.x * ROWS; i0 < b; i0 += (int)gridDim.x * ROWS, turn ^= 1) {
+        const int i = i0 + group;
+        const bool in = i < b;
+        RowShare<LANES, V> row = mine;
+        if (!in) row.whole = row.rest = 0;
+        const size_t at = (size_t)(in ? i : 0) * d;
+        float gx[G][V], n[G][V], last_g, last_n, su = 0.f, sn = 0.f;
+        const float mean = in ? mean_in[i] : 0.f, rstd = in ? rstd_in[i] : 0.f;
+        row.load(grad_x + at, gx, last_g, 0.f);
+        row.load(h + at, n, last_n, 0.f);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float w[V], t = 0.f, q = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) w[e] = 1.f;
+            if (gamma) row.load_group(gamma, g, w, 0.f);   // (from the L1: kept across the rows they would cost the registers that the sums need)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                n[g][e] = (n[g][e] - mean) * rstd;
+                sg[g][e] = fmaf(gx[g][e], n[g][e], sg[g][e]);
+                sb[g][e] += gx[g][e];
+                gx[g][e] *= w[e];   // u
+                t += gx[g][e];
+                q = fmaf(gx[g][e], n[g][e], q);
+            }
+            su += t;
+            sn += q;
+        }
+        last_n = (last_n - mean) * rstd;
+        last_sg = fmaf(last_g, last_n, last_sg);
+        last_sb += last_g;
+        if (gamma && row.has_rest()) last_g *= gamma[row.whole + row.lane];
+        su = sum_lanes<LANES>(su + last_g);
+        sn = sum_lanes<LANES>(fmaf(last_g, last_n, sn));
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) {
+                part[turn][0][threadIdx.x >> 6] = su;
+                part[turn][1][threadIdx.x >> 6] = sn;
+            }
+            __syncthreads();   // (two sets in turn: a set is written again behind the next barrier, which all reach behind their reads)
+            su = sn = 0.f;
+#pragma unroll
+            for (int q = 0; q < WAVES; ++q) {
+                su += part[turn][0][group * WAVES + q];
+                sn += part[turn][1][group * WAVES + q];
+            }
+        }
+        const float mu = su / (float)d, mn = sn / (float)d;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float o[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = rstd * (gx[g][e] - mu - n[g][e] * mn);
+            if (row.has(g)) store_vec(grad_h + at + row.at(g), o);
+        }
+        if (row.has_rest()) grad_h[at + row.whole + row.lane] = rstd * (last_g - mu - last_n * mn);
+    }
+    if (!to_gamma && !to_beta) return;
+#pragma unroll 1
+    for (int half = ROWS / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        float* both = lds + (size_t)(group % half) * (2 * (EPL + 1) * LANES) + mine.lane;
+        if (group >= half && group < 2 * half) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    both[(g * V + e) * LANES] = sg[g][e];
+                    both[(EPL + 1 + g * V + e) * LANES] = sb[g][e];
+                }
+            both[EPL * LANES] = last_sg;
+            both[(2 * EPL + 1) * LANES] = last_sb;
+        }
+        __syncthreads();
+        if (group < half) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sg[g][e] += both[(g * V + e) * LANES];
+                    sb[g][e] += both[(EPL + 1 + g * V + e) * LANES];
+                }
+            last_sg += both[EPL * LANES];
+            last_sb += both[(2 * EPL + 1) * LANES];
+        }
+    }
+    if (group > 0) return;
+    float* rows[2] = {to_gamma ? to_gamma + blockIdx.x * stride : nullptr, to_beta ? to_beta + blockIdx.x * stride : nullptr};
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (!rows[which]) continue;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (mine.has(g)) store_vec(rows[which] + mine.at(g), which ? sb[g] : sg[g]);
+        if (mine.has_rest()) rows[which][mine.whole + mine.lane] = which ? last_sb : last_sg;
+    }
+}
+
+// ---- backward, wide rows: the rows' sums first, then tiles of columns and rows -----------------------------------
+// The inputs are read twice, the second time mostly from the cache behind the L2s.
+// sums[i][split][2]: sums of u and u n over a share of row i's columns.  grid (splits, rows)
+constexpr int SUMS_NT = 512;
 template <typename TS>
-__global__ void __launch_bounds__(ANY_NT)
-k_norm_grad_any(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
-                const float* __restrict__ rstd_in, float* __restrict__ grad_h, int d) {
-    __shared__ double red[ANY_NT / 64];
-    const size_t at = (size_t)blockIdx.x * d;
-    const float mean = mean_in[blockIdx.x], rstd = rstd_in[blockIdx.x];
+__global__ void __launch_bounds__(SUMS_NT)
+k_norm_grad_sums(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
+                 const float* __restrict__ rstd_in, float* __restrict__ sums, int d, int cols) {
+    constexpr int V = VEC<TS>, AHEAD = 16 / V;
+    __shared__ double red[SUMS_NT / 64];
+    const float* gx_row = grad_x + (size_t)blockIdx.y * d;
+    const float mean = mean_in[blockIdx.y], rstd = rstd_in[blockIdx.y];
+    const TS* h_row = h + (size_t)blockIdx.y * d;
+    const int c0 = (int)blockIdx.x * cols, whole = d / V * V, end = min(whole, c0 + cols);
     double su = 0.0, sn = 0.0;
-    for (int c = threadIdx.x; c < d; c += ANY_NT) {
-        const float u = grad_x[at + c] * (gamma ? gamma[c] : 1.f), n = (usl_load_f32<TS>(h, at + c) - mean) * rstd;
+    for (int c = c0 + (int)threadIdx.x * V; c < end; c += SUMS_NT * V * AHEAD) {
+        float gx[AHEAD][V], v[AHEAD][V], w[AHEAD][V], t = 0.f, q = 0.f;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int ca = min(c + a * SUMS_NT * V, end - V);   // (behind the end: the last group once more, and nothing is made of it)
+            load_vec(gx_row + ca, gx[a]);
+            load_vec(h_row + ca, v[a]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) w[a][e] = 1.f;
+            if (gamma) load_vec(gamma + ca, w[a]);
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            float ta = 0.f, qa = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float u = gx[a][e] * w[a][e];
+                ta += u;
+                qa = fmaf(u, (v[a][e] - mean) * rstd, qa);
+            }
+            t += c + a * SUMS_NT * V < end ? ta : 0.f;
+            q += c + a * SUMS_NT * V < end ? qa : 0.f;
+        }
+        su += t;
+        sn += q;
+    }
+    if (blockIdx.x == 0 && (int)threadIdx.x < d - whole) {   // the values behind the whole groups
+        const int c = whole + (int)threadIdx.x;
+        const float u = gamma ? gx_row[c] * gamma[c] : gx_row[c];
         su += u;
-        sn += (double)u * n;
+        sn += (double)u * ((usl_to_f32(h_row[c]) - mean) * rstd);
     }
-    const float mu = (float)(block_sum<ANY_NT>(su, red) / d), mn = (float)(block_sum<ANY_NT>(sn, red) / d);
-    for (int c = threadIdx.x; c < d; c += ANY_NT) {
-        const float u = grad_x[at + c] * (gamma ? gamma[c] : 1.f), n = (usl_load_f32<TS>(h, at + c) - mean) * rstd;
-        grad_h[at + c] = rstd * (u - mu - n * mn);
+    const double all = block_sum<SUMS_NT>(su, red), alln = block_sum<SUMS_NT>(sn, red);
+    if (threadIdx.x == 0) {
+        float* to = sums + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 2;
+        to[0] = (float)all;
+        to[1] = (float)alln;
     }
 }
 
-// ---- the sums over the rows ------------------------------------------------------------------------------------
-// part[p][0][c] and part[p][1][c]: sums of grad_x n and of grad_x over the rows [p * rows, p * rows + rows).  A lane a column.
+// grad_h of a tile, and the tile's sums of grad_x n and grad_x over its rows into part[blockIdx.y][2][d].  A lane has 4 columns.  grid (columns, rows)
+constexpr int TILE_NT = 256, TILE_COLS = TILE_NT * 4, TILE_AT_ONCE = 4, TILE_ROWS = 2048 /* their statistics take 32 KB of LDS */;
+__device__ __forceinline__ void load_four(const float* p, float (&v)[4]) { load_vec(p, v); }
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void load_four(const uint16_t* p, float (&v)[4]) {
+    const u16x4 q = *reinterpret_cast<const u16x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = usl_bf16_to_f32(q[e]);
+}
 template <typename TS>
-__global__ void __launch_bounds__(256)
-k_norm_columns(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ mean, const float* __restrict__ rstd,
-               float* __restrict__ part, int b, int d, int rows) {
-    const int c = blockIdx.x * 256 + threadIdx.x, i0 = blockIdx.y * rows, i1 = min(b, i0 + rows);
-    if (c >= d) return;
-    float sg = 0.f, sb = 0.f;
-    for (int i = i0; i < i1; ++i) {
-        const float g = grad_x[(size_t)i * d + c];
-        sg = fmaf(g, (usl_load_f32<TS>(h, (size_t)i * d + c) - mean[i]) * rstd[i], sg);
-        sb += g;
+__global__ void __launch_bounds__(TILE_NT)
+k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
+                 const float* __restrict__ rstd_in, const float* __restrict__ sums, int splits, float* __restrict__ grad_h, float* __restrict__ part, int b, int d,
+                 int rows) {
+    extern __shared__ __align__(16) float of_row[];   // [rows][4]: mean, rstd, mean of u, mean of u n
+    const int i0 = (int)blockIdx.y * rows, n = min(rows, b - i0), lane = threadIdx.x & 63;
+    for (int r = (int)(threadIdx.x >> 6); r < n; r += TILE_NT / 64) {
+        float su = 0.f, sn = 0.f;
+        for (int s = lane; s < splits; s += 64) {
+            const float* from = sums + ((size_t)(i0 + r) * splits + s) * 2;
+            su += from[0];
+            sn += from[1];
+        }
+        su = sum64(su);
+        sn = sum64(sn);
+        if (lane == 0) {
+            of_row[r * 4] = mean_in[i0 + r];
+            of_row[r * 4 + 1] = rstd_in[i0 + r];
+            of_row[r * 4 + 2] = su / (float)d;
+            of_row[r * 4 + 3] = sn / (float)d;
+        }
     }
-    part[((size_t)blockIdx.y * 2) * d + c] = sg;
-    part[((size_t)blockIdx.y * 2 + 1) * d + c] = sb;
+    __syncthreads();
+    const int c = (int)blockIdx.x * TILE_COLS + (int)threadIdx.x * 4;
+    if (c >= d) return;
+    const bool full = c + 4 <= d;
+    float w[4] = {1.f, 1.f, 1.f, 1.f}, sg[4] = {}, sb[4] = {};
+    if (gamma) {
+        if (full) load_vec(gamma + c, w);
+        else
+            for (int e = 0; e < 4; ++e) w[e] = c + e < d ? gamma[c + e] : 0.f;
+    }
+    auto put = [&](float* to, const float (&o)[4]) {
+        if (full) store_vec(to + c, o);
+        else
+            for (int e = 0; e < 4; ++e)
+                if (c + e < d) to[c + e] = o[e];
+    };
+    for (int r0 = 0; r0 < n; r0 += TILE_AT_ONCE) {
+        float gx[TILE_AT_ONCE][4], v[TILE_AT_ONCE][4];
+#pragma unroll
+        for (int a = 0; a < TILE_AT_ONCE; ++a) {
+            const int r = min(r0 + a, n - 1);
+            const size_t at = (size_t)(i0 + r) * d;
+            if (full) {
+                load_four(grad_x + at + c, gx[a]);
+                load_four(h + at + c, v[a]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    gx[a][e] = c + e < d ? grad_x[at + c + e] : 0.f;
+                    v[a][e] = c + e < d ? usl_to_f32(h[at + c + e]) : 0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < TILE_AT_ONCE; ++a) {
+            if (r0 + a >= n) break;
+            const float4 k = *reinterpret_cast<const float4*>(of_row + (r0 + a) * 4);
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float u = gx[a][e] * w[e], m = (v[a][e] - k.x) * k.y;
+                o[e] = k.y * (u - k.z - m * k.w);
+                sg[e] = fmaf(gx[a][e], m, sg[e]);
+                sb[e] += gx[a][e];
+            }
+            put(grad_h + (size_t)(i0 + r0 + a) * d, o);
+        }
+    }
+    if (!part) return;
+    put(part + ((size_t)blockIdx.y * 2) * d, sg);
+    put(part + ((size_t)blockIdx.y * 2 + 1) * d, sb);
 }
 
-// ... added up in a fixed order.  grid (columns, 2)
-__global__ void __launch_bounds__(256)
+// The parts' sums, added up in a fixed order: 64 columns of [2][d] a workgroup, a sixteenth of the parts a wavefront.
+__global__ void __launch_bounds__(1024)
 k_norm_sum_parts(const float* __restrict__ part, int parts, int d, float* __restrict__ grad_gamma, float* __restrict__ grad_beta) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
+    __shared__ float red[16][64];
+    const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
     float* to = blockIdx.y ? grad_beta : grad_gamma;
-    if (c >= d || !to) return;
+    if (!to) return;
     float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += part[((size_t)p * 2 + blockIdx.y) * d + c];
-    to[c] = s;
+    if (col < d) {
+#pragma unroll 4
+        for (int p = wave; p < parts; p += 16) s += part[((size_t)p * 2 + blockIdx.y) * d + col];
+    }
+    red[wave][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (wave || col >= d) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += red[w][threadIdx.x];
+    to[col] = s;
 }
 
 }  // namespace
 
+// Lanes of a row by its length: 16 where four rows fit a wavefront, then a wavefront, then as many as keep 16 values each; the longest rows of a
+// workgroup have 32 or 64 values a lane.
 template <typename TS>
 static usl_status norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b) {
-    hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d);
+#define USL_NORM(LANES, EPL)                                                                                                        \
+    hipLaunchKernelGGL((k_norm<TS, LANES, EPL>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
+                       dim3(LANES < 256 ? 256 : LANES), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, b, c->d)
+    if (c->d <= 128) USL_NORM(16, 8);
+    else if (c->d <= 256) USL_NORM(16, 16);
+    else if (c->d <= 512) USL_NORM(64, 8);
+    else if (c->d <= 1024) USL_NORM(64, 16);
+    else if (c->d <= 2048) USL_NORM(64, 32);
+    else if (c->d <= 4096) USL_NORM(256, 16);
+    else if (c->d <= 8192) USL_NORM(512, 16);
+    else if (c->d <= 16384) USL_NORM(1024, 16);
+    else if (c->d <= 32768) USL_NORM(1024, 32);
+    else if (c->d <= 65536) USL_NORM(1024, 64);
+    else hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d);
+#undef USL_NORM
     return usl_check_launch(c, "layer_norm");
 }
 
@@ -114,25 +531,75 @@ usl_status usl_launch_norm(usl_ctx* c, const void* h, const float* gamma, const 
     return c->storage == USL_F32 ? norm<float>(c, h, gamma, beta, eps, x, mean, rstd, b) : norm<uint16_t>(c, h, gamma, beta, eps, x, mean, rstd, b);
 }
 
-// Parts that the rows of a batch are summed in: enough for four workgroups to a compute unit, at least 8 rows each.
-static int norm_rows_of_part(const usl_ctx* c, int b) {
-    const int tiles = (c->d + 255) / 256, want = (c->num_cu * 4 + tiles - 1) / tiles;
-    int rows = (b + want - 1) / want;
-    return rows < 8 ? 8 : rows;
+// How the backward pass is cut up.
+struct NormShape {
+    bool registers;   // rows in registers, one pass
+    int lanes, parts; // lanes of a row; sets of sums over rows
+    int rows, splits; // two passes: rows of a tile, shares of a row
+};
+static NormShape norm_shape(const usl_ctx* c, int b) {
+    NormShape s = {};
+    const int d = c->d, es = c->storage == USL_F32 ? 4 : 2;
+    s.lanes = d <= 128 ? 16 : d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
+    const int at_once = BWD_NT / s.lanes, all = (b + at_once - 1) / at_once;
+    s.parts = all < c->num_cu ? all : c->num_cu;
+    // The sums that a workgroup leaves are written and read once: 16 bytes a column and workgroup, against 4 + es bytes a value for reading the inputs again.
+    s.registers = d <= 16384 && (s.parts == 1 || (int64_t)s.parts * 16 <= (int64_t)b * (4 + es));
+    if (s.registers) return s;
+    const int tiles = (d + TILE_COLS - 1) / TILE_COLS, want = (c->num_cu * 2 + tiles - 1) / tiles;
+    s.rows = (b + want - 1) / want;
+    s.rows = s.rows < 8 ? 8 : s.rows > TILE_ROWS ? TILE_ROWS : s.rows;
+    s.parts = (b + s.rows - 1) / s.rows;
+    const int most = (d + 4095) / 4096;
+    s.splits = (c->num_cu * 2 + b - 1) / b;
+    if (s.splits > most) s.splits = most;
+    return s;
 }
 
 template <typename TS>
 static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, const float* gamma, const float* mean, const float* rstd, float* grad_h,
                             float* grad_gamma, float* grad_beta, int32_t b) {
-    if (grad_gamma || grad_beta) {
-        const int rows = norm_rows_of_part(c, b), parts = (b + rows - 1) / rows;
-        const int most = (c->max_b + 7) / 8 < c->num_cu * 4 ? (c->max_b + 7) / 8 : c->num_cu * 4;   // of any batch: no later call grows it
-        USL_TRY(usl_reserve(c, (void**)&c->norm_part, &c->norm_part_cap, (size_t)(most > parts ? most : parts) * 2 * c->d * 4));
-        const unsigned tiles = (unsigned)((c->d + 255) / 256);
-        hipLaunchKernelGGL(k_norm_columns<TS>, dim3(tiles, (unsigned)parts), dim3(256), 0, c->stream, grad_x, (const TS*)h, mean, rstd, c->norm_part, b, c->d, rows);
-        hipLaunchKernelGGL(k_norm_sum_parts, dim3(tiles, 2), dim3(256), 0, c->stream, c->norm_part, parts, c->d, grad_gamma, grad_beta);
+    const NormShape s = norm_shape(c, b);
+    const int d = c->d;
+    const bool sums = grad_gamma || grad_beta;
+    // scratch for any batch up to max_b: at most parts_most sets of sums, and max_b + 2 num_cu pairs of a row's sums
+    const int tiles = (d + TILE_COLS - 1) / TILE_COLS, want = (c->num_cu * 2 + tiles - 1) / tiles;
+    const int by_tiles = want > (c->max_b + TILE_ROWS - 1) / TILE_ROWS ? want : (c->max_b + TILE_ROWS - 1) / TILE_ROWS;
+    const int parts_most = d <= 16384 && by_tiles < c->num_cu ? c->num_cu : by_tiles;
+    const size_t held = (size_t)(parts_most < c->max_b ? parts_most : c->max_b) * 2 * d;
+    if (!s.registers || (sums && s.parts > 1))
+        USL_TRY(usl_reserve(c, (void**)&c->norm_part, &c->norm_part_cap, (held + 2 * ((size_t)c->max_b + 2 * c->num_cu)) * 4));
+    if (s.registers) {
+        const bool direct = s.parts == 1;
+        float* to_gamma = !sums ? nullptr : direct ? grad_gamma : c->norm_part;
+        float* to_beta = !sums ? nullptr : direct ? grad_beta : c->norm_part + d;
+#define USL_NORM_GRAD(LANES, EPL)                                                                                                                      \
+    do {                                                                                                                                               \
+        constexpr size_t lds = (size_t)(BWD_NT / LANES / 2) * 2 * (EPL + 1) * LANES * 4;                                                                      \
+        if (lds >= 65536)                                                                                                                              \
+            USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(k_norm_grad<TS, LANES, EPL>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
+        hipLaunchKernelGGL((k_norm_grad<TS, LANES, EPL>), dim3((unsigned)s.parts), dim3(BWD_NT), lds, c->stream, grad_x, (const TS*)h, gamma, mean,     \
+                           rstd, grad_h, to_gamma, to_beta, (size_t)2 * d, b, d);                                                                      \
+    } while (0)
+        if (d <= 128) USL_NORM_GRAD(16, 8);
+        else if (d <= 512) USL_NORM_GRAD(64, 8);
+        else if (d <= 1024) USL_NORM_GRAD(64, 16);
+        else if (d <= 4096) USL_NORM_GRAD(256, 16);
+        else if (d <= 8192) USL_NORM_GRAD(512, 16);
+        else USL_NORM_GRAD(1024, 16);
+#undef USL_NORM_GRAD
+        USL_TRY(usl_check_launch(c, "layer_norm_backward"));
+        if (!sums || direct) return USL_OK;
+    } else {
+        float* row_sums = c->norm_part + held;
+        const int cols = ((d + s.splits - 1) / s.splits + 15) / 16 * 16;
+        hipLaunchKernelGGL(k_norm_grad_sums<TS>, dim3((unsigned)s.splits, (unsigned)b), dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
+        hipLaunchKernelGGL(k_norm_grad_tile<TS>, dim3((unsigned)tiles, (unsigned)s.parts), dim3(TILE_NT), (size_t)s.rows * 16, c->stream, grad_x, (const TS*)h, gamma,
+                           mean, rstd, row_sums, s.splits, grad_h, sums ? c->norm_part : nullptr, b, d, s.rows);
+        USL_TRY(usl_check_launch(c, "layer_norm_backward"));
+        if (!sums) return USL_OK;
     }
-    hipLaunchKernelGGL(k_norm_grad_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, grad_h, c->d);
+    hipLaunchKernelGGL(k_norm_sum_parts, dim3((unsigned)((d + 63) / 64), 2), dim3(1024), 0, c->stream, c->norm_part, s.parts, d, grad_gamma, grad_beta);
     return usl_check_launch(c, "layer_norm_backward");
 }
 
