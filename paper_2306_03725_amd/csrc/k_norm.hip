@@ -46,30 +46,22 @@ __device__ __forceinline__ void store_vec(uint16_t* p, const float (&v)[8]) {
     *reinterpret_cast<u16x8*>(p) = q;
 }
 
-// How LANES lanes divide a row of d values: the whole groups of V values are dealt to the lanes in turn, the values behind them (fewer than V) go one to a lane.
-// (With the last group taken value by value every load and store has V branches, and the kernels spill.)
+// How LANES lanes divide a row of d >= V values: the whole groups of V values are dealt to the lanes in turn, the values behind them (fewer than V) go one
+// to a lane.  A lane without a group loads the row's last one instead, and leaves it out of its sums: a load under a lane's condition is waited for by the
+// compiler then and there.  (With the last group taken value by value every load and store had V branches, and the kernels spilled.)
 template <int LANES, int V>
 struct RowShare {
     int lane, whole, rest;   // values in whole groups, values behind them
     __device__ __forceinline__ RowShare(int lane_, int d) : lane(lane_), whole(d / V * V), rest(d % V) {}
+    // the lane number taken afresh: what is derived from it is rebuilt with a few instructions instead of living in registers that the row needs
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(lane)); }
     __device__ __forceinline__ int at(int g) const { return (g * LANES + lane) * V; }
     __device__ __forceinline__ bool has(int g) const { return at(g) < whole; }
     __device__ __forceinline__ bool has_rest() const { return lane < rest; }
-    template <typename T, int G>
-    __device__ __forceinline__ void load(const T* __restrict__ row, float (&v)[G][V], float& last, float fill) const {
-#pragma unroll
-        for (int g = 0; g < G; ++g) load_group(row, g, v[g], fill);
-        last = has_rest() ? usl_to_f32(row[whole + lane]) : fill;
-    }
     template <typename T>
-    __device__ __forceinline__ void load_group(const T* __restrict__ row, int g, float (&v)[V], float fill) const {
-        if (has(g)) {
-            load_vec(row + at(g), v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = fill;
-        }
-    }
+    __device__ __forceinline__ void load(const T* row, int g, float (&v)[V]) const { load_vec(row + min(at(g), whole - V), v); }
+    template <typename T>
+    __device__ __forceinline__ float load_rest(const T* row) const { return usl_to_f32(row[min(whole + lane, whole + rest - 1)]); }
 };
 
 // ---- sums over lanes --------------------------------------------------------------------------------------------
@@ -108,35 +100,38 @@ __device__ __forceinline__ T block_sum(T v, T* red) {
 // ---- forward: a row in the registers of LANES lanes, EPL values each (and one of the values behind the groups) --
 // Read once, written once.  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
 // around the row's mean, behind one barrier:  M2 = sum_w M2_w + n_w (mean_w - mean)^2.
-template <typename TS, int LANES, int EPL>
+// FULL: there are both a weight and a bias.
+template <typename TS, int LANES, int EPL, bool FULL>
 __global__ void __launch_bounds__((LANES < 256 ? 256 : LANES))
 k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, TS* x /* may be h */, float* __restrict__ mean_out,
        float* __restrict__ rstd_out, int b, int d) {
     constexpr int V = VEC<TS>, G = EPL / V, NT = LANES < 256 ? 256 : LANES, WAVES = LANES / 64;
-    constexpr bool EARLY = EPL <= 16;   // weight and bias come with the row; more registers than that are not left
+    constexpr bool EARLY = FULL && EPL <= 16;   // weight and bias come with the row; more registers than that are not left
     int i = (int)blockIdx.x * (NT / LANES) + (int)threadIdx.x / LANES;
     if (LANES >= 64) i = __builtin_amdgcn_readfirstlane(i);
     if (i >= b) return;   // (rows of several wavefronts have a workgroup each)
-    const RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
-    float v[G][V], last, wg[EARLY ? G : 1][V], wb[EARLY ? G : 1][V];
-    mine.load(h + (size_t)i * d, v, last, 0.f);
+    RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
+    float v[G][V], wg[EARLY ? G : 1][V], wb[EARLY ? G : 1][V];
+    const TS* from = h + (size_t)i * d;
+#pragma unroll
+    for (int g = 0; g < G; ++g) mine.load(from, g, v[g]);
+    float last = mine.load_rest(from);
+    if (!mine.has_rest()) last = 0.f;
     if constexpr (EARLY) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) { wg[g][e] = 1.f; wb[g][e] = 0.f; }
-            if (gamma) mine.load_group(gamma, g, wg[g], 0.f);
-            if (beta) mine.load_group(beta, g, wb[g], 0.f);
+            mine.load(gamma, g, wg[g]);
+            mine.load(beta, g, wb[g]);
         }
     }
-    const float last_w = gamma && mine.has_rest() ? gamma[mine.whole + mine.lane] : 1.f, last_b = beta && mine.has_rest() ? beta[mine.whole + mine.lane] : 0.f;
+    const float last_w = gamma ? mine.load_rest(gamma) : 1.f, last_b = beta ? mine.load_rest(beta) : 0.f;
     float s = last;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         float t = v[g][0];
 #pragma unroll
         for (int e = 1; e < V; ++e) t += v[g][e];
-        s += t;
+        s += mine.has(g) ? t : 0.f;
     }
     int n = d;   // values of this wavefront
     if (LANES > 64) {
@@ -180,6 +175,7 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
         if (rstd_out) rstd_out[i] = rstd;
     }
     TS* to = x + (size_t)i * d;
+    mine.renew();
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         float o[V], w[V], c[V];
@@ -189,8 +185,8 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) { w[e] = 1.f; c[e] = 0.f; }
-            if (gamma) mine.load_group(gamma, g, w, 0.f);
-            if (beta) mine.load_group(beta, g, c, 0.f);
+            if (FULL || gamma) mine.load(gamma, g, w);
+            if (FULL || beta) mine.load(beta, g, c);
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] = fmaf((v[g][e] - mean) * rstd, w[e], c[e]);
@@ -230,17 +226,17 @@ k_norm_any(const TS* h, const float* __restrict__ gamma, const float* __restrict
 
 // ---- backward, rows of up to 16384: a row in the registers of LANES lanes, EPL values each -----------------------
 // A workgroup of 1024 lanes takes 1024 / LANES rows at a time, its share of the batch one after the other, and keeps the sums of grad_x n and grad_x
-// of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined pairwise through LDS, always in the same order,
-// and left in part[workgroup][2][d] (with one workgroup: in the gradients themselves).
+// of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined through LDS, always in the same order, and left in part[workgroup][2][d] (with one workgroup: in the gradients themselves).
+// WEIGHT: there is a gamma.
 constexpr int BWD_NT = 1024;
-template <typename TS, int LANES, int EPL>
+template <typename TS, int LANES, int EPL, bool WEIGHT>
 __global__ void __launch_bounds__(BWD_NT)
 k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
             const float* __restrict__ rstd_in, float* __restrict__ grad_h, float* __restrict__ to_gamma, float* __restrict__ to_beta, size_t stride, int b, int d) {
     constexpr int V = VEC<TS>, G = EPL / V, ROWS = BWD_NT / LANES, WAVES = LANES / 64;
-    extern __shared__ __align__(16) float lds[];   // [ROWS / 2][2][EPL + 1][LANES]
+    extern __shared__ __align__(16) float lds[];   // [ROWS][2][EPL + 1][LANES], with one row none
     __shared__ float part[2][2][BWD_NT / 64];
-    const RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
+    RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
     int group = (int)threadIdx.x / LANES;
     if (LANES >= 64) group = __builtin_amdgcn_readfirstlane(group);
     float sg[G][V] = {}, sb[G][V] = {}, last_sg = 0.f, last_sb = 0.f;
@@ -248,35 +244,43 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
     for (int i0 = (int)blockIdx.x * ROWS; i0 < b; i0 += (int)gridDim.x * ROWS, turn ^= 1) {
         const int i = i0 + group;
         const bool in = i < b;
-        RowShare<LANES, V> row = mine;
-        if (!in) row.whole = row.rest = 0;
-        const size_t at = (size_t)(in ? i : 0) * d;
-        float gx[G][V], n[G][V], last_g, last_n, su = 0.f, sn = 0.f;
-        const float mean = in ? mean_in[i] : 0.f, rstd = in ? rstd_in[i] : 0.f;
-        row.load(grad_x + at, gx, last_g, 0.f);
-        row.load(h + at, n, last_n, 0.f);
+        mine.renew();
+        const size_t at = (size_t)(in ? i : 0) * d;   // (a row group without a row takes row 0, and adds nothing)
+        float gx[G][V], n[G][V], su = 0.f, sn = 0.f;
+        const float mean = mean_in[in ? i : 0], rstd = rstd_in[in ? i : 0];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            mine.load(grad_x + at, g, gx[g]);
+            mine.load(h + at, g, n[g]);
+        }
+        float last_g = mine.load_rest(grad_x + at), last_n = mine.load_rest(h + at);
+        if (!in || !mine.has_rest()) last_g = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float w[V], t = 0.f, q = 0.f;
+            if (WEIGHT) mine.load(gamma, g, w);   // (from the L1: kept across the rows they would cost the registers that the sums need)
+            if (G > 2 && g % 2) __builtin_amdgcn_sched_barrier(0);   // two groups' at a time
+            if (!in) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) w[e] = 1.f;
-            if (gamma) row.load_group(gamma, g, w, 0.f);   // (from the L1: kept across the rows they would cost the registers that the sums need)
+                for (int e = 0; e < V; ++e) gx[g][e] = 0.f;
+            }
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
+            for (int e = 0; e < V; ++e) {   // (a lane without the group: its sums of columns go nowhere)
                 n[g][e] = (n[g][e] - mean) * rstd;
                 sg[g][e] = fmaf(gx[g][e], n[g][e], sg[g][e]);
                 sb[g][e] += gx[g][e];
-                gx[g][e] *= w[e];   // u
+                if (WEIGHT) gx[g][e] *= w[e];   // u
                 t += gx[g][e];
                 q = fmaf(gx[g][e], n[g][e], q);
             }
-            su += t;
-            sn += q;
+            su += mine.has(g) ? t : 0.f;
+            sn += mine.has(g) ? q : 0.f;
         }
         last_n = (last_n - mean) * rstd;
         last_sg = fmaf(last_g, last_n, last_sg);
         last_sb += last_g;
-        if (gamma && row.has_rest()) last_g *= gamma[row.whole + row.lane];
+        if (WEIGHT) last_g *= mine.load_rest(gamma);
+        if (!mine.has_rest()) last_g = last_n = 0.f;
         su = sum_lanes<LANES>(su + last_g);
         sn = sum_lanes<LANES>(fmaf(last_g, last_n, sn));
         if constexpr (LANES > 64) {
@@ -293,53 +297,49 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
             }
         }
         const float mu = su / (float)d, mn = sn / (float)d;
+        mine.renew();
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) o[e] = rstd * (gx[g][e] - mu - n[g][e] * mn);
-            if (row.has(g)) store_vec(grad_h + at + row.at(g), o);
+            if (in && mine.has(g)) store_vec(grad_h + at + mine.at(g), o);
         }
-        if (row.has_rest()) grad_h[at + row.whole + row.lane] = rstd * (last_g - mu - last_n * mn);
+        if (in && mine.has_rest()) grad_h[at + mine.whole + mine.lane] = rstd * (last_g - mu - last_n * mn);
     }
     if (!to_gamma && !to_beta) return;
-#pragma unroll 1
-    for (int half = ROWS / 2; half > 0; half >>= 1) {
-        __syncthreads();
-        float* both = lds + (size_t)(group % half) * (2 * (EPL + 1) * LANES) + mine.lane;
-        if (group >= half && group < 2 * half) {
+    if constexpr (ROWS == 1) {
+        float* rows[2] = {to_gamma ? to_gamma + blockIdx.x * stride : nullptr, to_beta ? to_beta + blockIdx.x * stride : nullptr};
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (!rows[which]) continue;
 #pragma unroll
             for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    both[(g * V + e) * LANES] = sg[g][e];
-                    both[(EPL + 1 + g * V + e) * LANES] = sb[g][e];
-                }
-            both[EPL * LANES] = last_sg;
-            both[(2 * EPL + 1) * LANES] = last_sb;
+                if (mine.has(g)) store_vec(rows[which] + mine.at(g), which ? sb[g] : sg[g]);
+            if (mine.has_rest()) rows[which][mine.whole + mine.lane] = which ? last_sb : last_sg;
         }
-        __syncthreads();
-        if (group < half) {
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    sg[g][e] += both[(g * V + e) * LANES];
-                    sb[g][e] += both[(EPL + 1 + g * V + e) * LANES];
-                }
-            last_sg += both[EPL * LANES];
-            last_sb += both[(2 * EPL + 1) * LANES];
-        }
-    }
-    if (group > 0) return;
-    float* rows[2] = {to_gamma ? to_gamma + blockIdx.x * stride : nullptr, to_beta ? to_beta + blockIdx.x * stride : nullptr};
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        if (!rows[which]) continue;
+    } else {   // every row group leaves its sums, and every lane joins those of a few columns
+        constexpr int E = EPL + 1, ENTRIES = 2 * E * LANES;   // [2][value of a lane, the rest][lane]
+        float* own = lds + group * ENTRIES + mine.lane;
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            if (mine.has(g)) store_vec(rows[which] + mine.at(g), which ? sb[g] : sg[g]);
-        if (mine.has_rest()) rows[which][mine.whole + mine.lane] = which ? last_sb : last_sg;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                own[(g * V + e) * LANES] = sg[g][e];
+                own[(E + g * V + e) * LANES] = sb[g][e];
+            }
+        own[EPL * LANES] = last_sg;
+        own[(E + EPL) * LANES] = last_sb;
+        __syncthreads();
+        for (int at = (int)threadIdx.x; at < ENTRIES; at += BWD_NT) {
+            float s = lds[at];
+#pragma unroll
+            for (int r = 1; r < ROWS; ++r) s += lds[r * ENTRIES + at];
+            const int lane = at % LANES, q = at / LANES % E;
+            float* to = at < E * LANES ? to_gamma : to_beta;
+            const int c = q == EPL ? mine.whole + lane : (q / V * LANES + lane) * V + q % V;
+            if (to && (q == EPL ? lane < mine.rest : c < mine.whole)) to[blockIdx.x * stride + c] = s;
+        }
     }
 }
 
@@ -347,7 +347,7 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
 // The inputs are read twice, the second time mostly from the cache behind the L2s.
 // sums[i][split][2]: sums of u and u n over a share of row i's columns.  grid (splits, rows)
 constexpr int SUMS_NT = 512;
-template <typename TS>
+template <typename TS, bool WEIGHT>
 __global__ void __launch_bounds__(SUMS_NT)
 k_norm_grad_sums(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
                  const float* __restrict__ rstd_in, float* __restrict__ sums, int d, int cols) {
@@ -365,16 +365,14 @@ k_norm_grad_sums(const float* __restrict__ grad_x, const TS* __restrict__ h, con
             const int ca = min(c + a * SUMS_NT * V, end - V);   // (behind the end: the last group once more, and nothing is made of it)
             load_vec(gx_row + ca, gx[a]);
             load_vec(h_row + ca, v[a]);
-#pragma unroll
-            for (int e = 0; e < V; ++e) w[a][e] = 1.f;
-            if (gamma) load_vec(gamma + ca, w[a]);
+            if (WEIGHT) load_vec(gamma + ca, w[a]);
         }
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             float ta = 0.f, qa = 0.f;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float u = gx[a][e] * w[a][e];
+                const float u = WEIGHT ? gx[a][e] * w[a][e] : gx[a][e];
                 ta += u;
                 qa = fmaf(u, (v[a][e] - mean) * rstd, qa);
             }
@@ -509,10 +507,13 @@ k_norm_sum_parts(const float* __restrict__ part, int parts, int d, float* __rest
 // workgroup have 32 or 64 values a lane.
 template <typename TS>
 static usl_status norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b) {
-#define USL_NORM(LANES, EPL)                                                                                                        \
-    hipLaunchKernelGGL((k_norm<TS, LANES, EPL>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
+#define USL_NORM(LANES, EPL) do { if (gamma && beta) USL_NORM_F(LANES, EPL, true); else USL_NORM_F(LANES, EPL, false); } while (0)
+#define USL_NORM_F(LANES, EPL, FULL)                                                                                                \
+    hipLaunchKernelGGL((k_norm<TS, LANES, EPL, FULL>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
                        dim3(LANES < 256 ? 256 : LANES), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, b, c->d)
-    if (c->d <= 128) USL_NORM(16, 8);
+#define USL_NORM_ANY hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d)
+    if (c->d < VEC<TS>) USL_NORM_ANY;
+    else if (c->d <= 128) USL_NORM(16, 8);
     else if (c->d <= 256) USL_NORM(16, 16);
     else if (c->d <= 512) USL_NORM(64, 8);
     else if (c->d <= 1024) USL_NORM(64, 16);
@@ -522,7 +523,9 @@ static usl_status norm(usl_ctx* c, const void* h, const float* gamma, const floa
     else if (c->d <= 16384) USL_NORM(1024, 16);
     else if (c->d <= 32768) USL_NORM(1024, 32);
     else if (c->d <= 65536) USL_NORM(1024, 64);
-    else hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d);
+    else USL_NORM_ANY;
+#undef USL_NORM_ANY
+#undef USL_NORM_F
 #undef USL_NORM
     return usl_check_launch(c, "layer_norm");
 }
@@ -544,7 +547,7 @@ static NormShape norm_shape(const usl_ctx* c, int b) {
     const int at_once = BWD_NT / s.lanes, all = (b + at_once - 1) / at_once;
     s.parts = all < c->num_cu ? all : c->num_cu;
     // The sums that a workgroup leaves are written and read once: 16 bytes a column and workgroup, against 4 + es bytes a value for reading the inputs again.
-    s.registers = d <= 16384 && (s.parts == 1 || (int64_t)s.parts * 16 <= (int64_t)b * (4 + es));
+    s.registers = d <= 16384 && d * es >= 16 && (s.parts == 1 || (int64_t)s.parts * 16 <= (int64_t)b * (4 + es));
     if (s.registers) return s;
     const int tiles = (d + TILE_COLS - 1) / TILE_COLS, want = (c->num_cu * 2 + tiles - 1) / tiles;
     s.rows = (b + want - 1) / want;
@@ -573,12 +576,13 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
         const bool direct = s.parts == 1;
         float* to_gamma = !sums ? nullptr : direct ? grad_gamma : c->norm_part;
         float* to_beta = !sums ? nullptr : direct ? grad_beta : c->norm_part + d;
-#define USL_NORM_GRAD(LANES, EPL)                                                                                                                      \
+#define USL_NORM_GRAD(LANES, EPL) do { if (gamma) USL_NORM_GRAD_W(LANES, EPL, true); else USL_NORM_GRAD_W(LANES, EPL, false); } while (0)
+#define USL_NORM_GRAD_W(LANES, EPL, WEIGHT)                                                                                                                      \
     do {                                                                                                                                               \
-        constexpr size_t lds = (size_t)(BWD_NT / LANES / 2) * 2 * (EPL + 1) * LANES * 4;                                                                      \
+        constexpr size_t lds = LANES == BWD_NT ? 0 : (size_t)BWD_NT * 2 * (EPL + 1) * 4;                                                                      \
         if (lds >= 65536)                                                                                                                              \
-            USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(k_norm_grad<TS, LANES, EPL>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
-        hipLaunchKernelGGL((k_norm_grad<TS, LANES, EPL>), dim3((unsigned)s.parts), dim3(BWD_NT), lds, c->stream, grad_x, (const TS*)h, gamma, mean,     \
+            USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(k_norm_grad<TS, LANES, EPL, WEIGHT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
+        hipLaunchKernelGGL((k_norm_grad<TS, LANES, EPL, WEIGHT>), dim3((unsigned)s.parts), dim3(BWD_NT), lds, c->stream, grad_x, (const TS*)h, gamma, mean,     \
                            rstd, grad_h, to_gamma, to_beta, (size_t)2 * d, b, d);                                                                      \
     } while (0)
         if (d <= 128) USL_NORM_GRAD(16, 8);
@@ -587,13 +591,16 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
         else if (d <= 4096) USL_NORM_GRAD(256, 16);
         else if (d <= 8192) USL_NORM_GRAD(512, 16);
         else USL_NORM_GRAD(1024, 16);
+#undef USL_NORM_GRAD_W
 #undef USL_NORM_GRAD
         USL_TRY(usl_check_launch(c, "layer_norm_backward"));
         if (!sums || direct) return USL_OK;
     } else {
         float* row_sums = c->norm_part + held;
         const int cols = ((d + s.splits - 1) / s.splits + 15) / 16 * 16;
-        hipLaunchKernelGGL(k_norm_grad_sums<TS>, dim3((unsigned)s.splits, (unsigned)b), dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
+        const dim3 grid((unsigned)s.splits, (unsigned)b);
+        if (gamma) hipLaunchKernelGGL((k_norm_grad_sums<TS, true>), grid, dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
+        else hipLaunchKernelGGL((k_norm_grad_sums<TS, false>), grid, dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
         hipLaunchKernelGGL(k_norm_grad_tile<TS>, dim3((unsigned)tiles, (unsigned)s.parts), dim3(TILE_NT), (size_t)s.rows * 16, c->stream, grad_x, (const TS*)h, gamma,
                            mean, rstd, row_sums, s.splits, grad_h, sums ? c->norm_part : nullptr, b, d, s.rows);
         USL_TRY(usl_check_launch(c, "layer_norm_backward"));

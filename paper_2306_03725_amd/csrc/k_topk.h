@@ -39,6 +39,17 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     v = max_with<0x143, 0xC>(v);
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t plus(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true); }   // (no source: 0)
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+    v = plus<0x111, 0xF>(v);
+    v = plus<0x112, 0xF>(v);
+    v = plus<0x114, 0xF>(v);
+    v = plus<0x118, 0xF>(v);
+    v = plus<0x142, 0xA>(v);
+    v = plus<0x143, 0xC>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
     const uint32_t hi = wave_max((uint32_t)(v >> 32)), lo = wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
     return (uint64_t)hi << 32 | lo;
