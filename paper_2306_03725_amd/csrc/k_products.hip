@@ -5,6 +5,7 @@
 
 #include "k_products.h"
 #include "k_products_common.h"
+#include "k_mx4_few.h"
 #include "k_count.h"
 #include "k_topk.h"
 
@@ -182,10 +183,6 @@ k_interleave(const TS* __restrict__ x, TS* __restrict__ xi, int b, int d, int co
     *reinterpret_cast<U*>(to) = u;
 }
 
-// v of another lane: a permutation within 16 lanes by the vector unit
-template <int CTRL>
-__device__ __forceinline__ float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
-
 // ---- forward of one group of instances (b <= Q) ----------------------------------------------------------------
 // With one row of activations nothing is reused, and bringing idx and W into registers label by label only delays them:
 // here they stream.  A lane takes four neighbouring slots (16 bytes of idx, 16 or 8 of W, coalesced), gathers their
@@ -205,13 +202,11 @@ __device__ __forceinline__ float moved(float v) { return __int_as_float(__builti
 // it takes 10 more registers, with which a compute unit holds one workgroup of 1024 in the place of two where k is no multiple of 4.  Where it is used:
 // best_from_forward.  (Several instances one after the other took longer than a kernel over the scores: m = 31k, d = 1k, k = 32, b = 4 16.2 and 26.6.)
 constexpr int FEW_HELD = 4;   // turns whose scores, or candidates, a lane keeps in registers
-// MX4: W are the codes of values in 4 bits (k_mx4.h).  Two lanes share a word of eight codes; a lane's four slots lie in one block, so its sum of
-// codes times activations is scaled once.
-template <int LPL, typename TS, int Q, bool VEC, int AHEAD, bool BEST, bool MX4 = false>
+template <int LPL, typename TS, int Q, bool VEC, int AHEAD, bool BEST>
 __global__ void __launch_bounds__(1024)
 k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS* __restrict__ W, float* __restrict__ out,
               int64_t m, int k, int b, int row_bytes, int rounds, int kk, uint64_t* __restrict__ cand, uint32_t* __restrict__ done,
-              int32_t* __restrict__ top_lab, float* __restrict__ top_val, const uint8_t* __restrict__ scales) {
+              int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
     typedef typename Unit<TS, Q>::T U;
     extern __shared__ __align__(16) unsigned char lds_raw[];
     const uint32_t lds0 = lds_base(lds_raw);
@@ -229,20 +224,7 @@ k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, cons
     auto fetch = [&](int64_t j0, int r, Piece& p) {
         const int64_t j = j0 + r * (64 / LPL) + lane / LPL;
         const bool in = j < m && t < k;
-        if constexpr (MX4) {
-            uint4 c = make_uint4(nowhere, nowhere, nowhere, nowhere);
-            if (VEC) {
-                if (in) c = *reinterpret_cast<const uint4*>(idx + j * k + t);
-            } else if (in) {
-                c.x = (uint32_t)idx[j * k + t];
-                if (t + 1 < k) c.y = (uint32_t)idx[j * k + t + 1];
-                if (t + 2 < k) c.z = (uint32_t)idx[j * k + t + 2];
-                if (t + 3 < k) c.w = (uint32_t)idx[j * k + t + 3];
-            }
-            p.c[0] = c.x; p.c[1] = c.y; p.c[2] = c.z; p.c[3] = c.w;
-            p.w[0] = in ? reinterpret_cast<const uint32_t*>(W)[j * mx4_words(k) + (t >> 3)] : 0u;
-            p.w[1] = in ? scales[j * mx4_blocks(k) + t / MX4_BLOCK] : 127u;
-        } else if (VEC) {
+        if (VEC) {
             uint4 c = make_uint4(nowhere, nowhere, nowhere, nowhere);
             if (in) c = *reinterpret_cast<const uint4*>(idx + j * k + t);
             p.c[0] = c.x; p.c[1] = c.y; p.c[2] = c.z; p.c[3] = c.w;
@@ -271,39 +253,7 @@ k_forward_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, cons
         U v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = activation(p.c[q]);
-        if constexpr (MX4) {
-            const uint32_t half = p.w[0] >> (16 * (sub & 1));
-            const float scale = mx4_scale(p.w[1]);
-#pragma unroll
-            for (int q = 0; q < 4; q += 2) {
-                if constexpr (sizeof(TS) == 4) {
-                    const f32x2 w = q ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 1) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 0);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        if constexpr (Q == 1) acc[0] = fmaf(w[u], v[q + u], acc[0]);
-                        else {
-#pragma unroll
-                            for (int i = 0; i < Q; ++i) acc[i] = fmaf(w[u], v[q + u][i], acc[i]);
-                        }
-                    }
-                } else {
-                    const uint32_t w = __builtin_bit_cast(uint32_t, q ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 1)
-                                                                     : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 0));
-                    if constexpr (Q == 1) acc[0] = dot2((uint32_t)v[q] | ((uint32_t)v[q + 1] << 16), w, acc[0]);
-                    else if constexpr (Q == 2) {
-                        acc[0] = dot2(join_lo(v[q], v[q + 1]), w, acc[0]);
-                        acc[1] = dot2(join_hi(v[q], v[q + 1]), w, acc[1]);
-                    } else {
-                        acc[0] = dot2(join_lo(v[q].x, v[q + 1].x), w, acc[0]);
-                        acc[1] = dot2(join_hi(v[q].x, v[q + 1].x), w, acc[1]);
-                        acc[2] = dot2(join_lo(v[q].y, v[q + 1].y), w, acc[2]);
-                        acc[3] = dot2(join_hi(v[q].y, v[q + 1].y), w, acc[3]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < Q; ++i) acc[i] *= scale;
-        } else if constexpr (sizeof(TS) == 4) {
+        if constexpr (sizeof(TS) == 4) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float w = __uint_as_float(p.w[q]);
@@ -878,9 +828,8 @@ bool last_one_merges(const usl_ctx* c, const FewShape& f, int kk) {
 }
 
 // One group of instances: the streaming kernel.  kk > 0, one instance: its best labels; out is scratch then, written only by wavefronts of more than FEW_HELD turns.
-// mx4: the scales of values in 4 bits, whose codes W are.
 usl_status run_forward_few(usl_ctx* c, const Layout& L, const void* x, const int32_t* idx, const void* W, float* out, int b, int kk = 0, int32_t* top_lab = nullptr,
-                           float* top_val = nullptr, const uint8_t* mx4 = nullptr) {
+                           float* top_val = nullptr) {
     const void* xi = nullptr;
     USL_TRY(activations(c, L, x, b, &xi));
     const FewShape f = few_shape(c, L, kk);
@@ -895,19 +844,14 @@ usl_status run_forward_few(usl_ctx* c, const Layout& L, const void* x, const int
         cand = c->topk_cand;
         merge = c->topk_done_clear && last_one_merges(c, f, kk);
     }
-#define USL_FEW_B(LPL, TS, Q, VEC, AHEAD, BEST, MX4)                                                               \
+#define USL_FEW_B(LPL, TS, Q, VEC, AHEAD, BEST)                                                                    \
     do {                                                                                                                \
-        USL_TRY(allow_lds(c, k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST, MX4>, lds));                               \
-        hipLaunchKernelGGL((k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST, MX4>), dim3(grid), dim3((unsigned)nw * 64), lds, c->stream,   \
+        USL_TRY(allow_lds(c, k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST>, lds));                                    \
+        hipLaunchKernelGGL((k_forward_few<LPL, TS, Q, VEC, AHEAD, BEST>), dim3(grid), dim3((unsigned)nw * 64), lds, c->stream,        \
                            (const char*)xi, idx, (const TS*)W, out, c->m, c->k, b, L.row_bytes, rounds, kk, cand,      \
-                           c->topk_done, merge ? top_lab : nullptr, top_val, mx4);                                                     \
+                           c->topk_done, merge ? top_lab : nullptr, top_val);                                                          \
     } while (0)
-#define USL_FEW_A(LPL, TS, Q, VEC, AHEAD)                                                                          \
-    do {                                                                                                                \
-        if (mx4) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false, true);                                                       \
-        else if (Q == 1 && kk > 0) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, (Q == 1), false);                                 \
-        else USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false, false);                                                          \
-    } while (0)
+#define USL_FEW_A(LPL, TS, Q, VEC, AHEAD) do { if (Q == 1 && kk > 0) USL_FEW_B(LPL, TS, Q, VEC, AHEAD, (Q == 1)); else USL_FEW_B(LPL, TS, Q, VEC, AHEAD, false); } while (0)
 #define USL_FEW(LPL, TS, Q, VEC)                                                                                    \
     do {                                                                                                                \
         if (Q == 1 && LPL >= 4 && rounds >= 4) USL_FEW_A(LPL, TS, Q, VEC, (Q == 1 && LPL >= 4 ? 4 : 2));            \
@@ -991,9 +935,7 @@ bool streams(const usl_ctx* c, const Layout& L, int b) { return b <= L.Q && !L.h
 }  // namespace
 
 // mx4: the scales of values in 4 bits, whose codes W are
-static usl_status forward_by_gathers(usl_ctx* c, const void* x, const int32_t* idx, const void* W, const uint8_t* mx4, float* out, int32_t b) {
-    const Layout L = layout_of(c, b, x);
-    if (streams(c, L, b)) return run_forward_few(c, L, x, idx, W, out, b, 0, nullptr, nullptr, mx4);
+static usl_status run_forward_all(usl_ctx* c, const Layout& L, const void* x, const int32_t* idx, const void* W, const uint8_t* mx4, float* out, int32_t b) {
     USL_TRY(run_forward(c, L, x, idx, W, out, b, LossArgs{-1, 0.f, nullptr, nullptr, nullptr, 0, nullptr}, nullptr, Before{}, mx4));
     if (!pads_with_column_0(c, L)) return USL_OK;
     const dim3 grid((unsigned)((c->m + 255) / 256));
@@ -1007,12 +949,61 @@ static usl_status forward_by_gathers(usl_ctx* c, const void* x, const int32_t* i
 usl_status usl_launch_forward(usl_ctx* c, const void* x, const int32_t* idx, const void* W, float* out, int32_t b) {
     if (!fast_path_ok(c, idx, W))
         return c->storage == USL_F32 ? run_forward_generic<float>(c, x, idx, W, out, b) : run_forward_generic<uint16_t>(c, x, idx, W, out, b);
-    return forward_by_gathers(c, x, idx, W, nullptr, out, b);
+    const Layout L = layout_of(c, b, x);
+    return streams(c, L, b) ? run_forward_few(c, L, x, idx, W, out, b) : run_forward_all(c, L, x, idx, W, nullptr, out, b);
+}
+
+// One group of instances: the streaming kernel.
+static usl_status run_mx4_few(usl_ctx* c, const Layout& L, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int b) {
+    const void* xi = nullptr;
+    const int lpl = c->k <= 8 ? 2 : c->k <= 16 ? 4 : c->k <= 32 ? 8 : 16;
+    if (c->m < 64 / lpl) return usl_launch_forward_mx4_any(c, x, idx, codes, scales, out, b);
+    // workgroups of 4 or 8 wavefronts where there are too few rounds for 16 on every compute unit
+    const int64_t rounds = (c->m * lpl + 63) / 64, cus = c->num_cu;
+    const int nw = rounds >= cus * 16 ? 16 : rounds >= cus * 8 ? 8 : 4;
+    const size_t lds = (size_t)L.row_bytes + 16;
+    const int by_lds = (int)((size_t)(160 * 1024) / lds), resident = by_lds < 32 / nw ? (by_lds < 1 ? 1 : by_lds) : 32 / nw;
+    const int64_t blocks = (rounds + nw - 1) / nw;
+    const unsigned grid = (unsigned)(blocks < cus * resident ? blocks : cus * resident);
+    USL_TRY(activations(c, L, x, b, &xi));
+#define USL_MX4_FEW(LPL, TS, Q, SLOTS, AHEAD)                                                                                                          \
+    do {                                                                                                                                               \
+        USL_TRY(allow_lds(c, k_mx4_few<LPL, TS, Q, SLOTS, AHEAD>, lds));                                                                               \
+        hipLaunchKernelGGL((k_mx4_few<LPL, TS, Q, SLOTS, AHEAD>), dim3(grid), dim3((unsigned)nw * 64), lds, c->stream, (const char*)xi, idx, codes,    \
+                           scales, out, c->m, c->k, b, L.row_bytes);                                                                                   \
+    } while (0)
+#define USL_MX4_FEW_S(LPL, TS, Q, AHEAD)                                               \
+    do {                                                                               \
+        if (c->k == 4 * LPL) USL_MX4_FEW(LPL, TS, Q, MX4_ALL_SLOTS, AHEAD);            \
+        else if (c->k % 4 == 0) USL_MX4_FEW(LPL, TS, Q, MX4_FOURS, AHEAD);             \
+        else USL_MX4_FEW(LPL, TS, Q, MX4_ANY_SLOTS, AHEAD);                            \
+    } while (0)
+#define USL_MX4_FEW_L(TS, Q)                                             \
+    do {                                                                 \
+        if (lpl == 2) USL_MX4_FEW_S(2, TS, Q, 2);                        \
+        else if (lpl == 4) USL_MX4_FEW_S(4, TS, Q, (Q == 1 ? 4 : 2));    \
+        else if (lpl == 8) USL_MX4_FEW_S(8, TS, Q, (Q == 1 ? 4 : 2));    \
+        else USL_MX4_FEW_S(16, TS, Q, (Q == 1 ? 4 : 2));                 \
+    } while (0)
+    if (c->storage == USL_F32) {
+        if (L.Q == 4) USL_MX4_FEW_L(float, 4);
+        else if (L.Q == 2) USL_MX4_FEW_L(float, 2);
+        else USL_MX4_FEW_L(float, 1);
+    } else {
+        if (L.Q == 4) USL_MX4_FEW_L(uint16_t, 4);
+        else if (L.Q == 2) USL_MX4_FEW_L(uint16_t, 2);
+        else USL_MX4_FEW_L(uint16_t, 1);
+    }
+#undef USL_MX4_FEW_L
+#undef USL_MX4_FEW_S
+#undef USL_MX4_FEW
+    return usl_check_launch(c, "forward_mx4 (one group)");
 }
 
 usl_status usl_launch_forward_mx4(usl_ctx* c, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b) {
     if (!fast_path_ok(c, idx, nullptr)) return usl_launch_forward_mx4_any(c, x, idx, codes, scales, out, b);
-    return forward_by_gathers(c, x, idx, codes, scales, out, b);
+    const Layout L = layout_of(c, b, x);
+    return streams(c, L, b) ? run_mx4_few(c, L, x, idx, codes, scales, out, b) : run_forward_all(c, L, x, idx, codes, scales, out, b);
 }
 
 usl_status usl_launch_predict_few(usl_ctx* c, const void* x, const int32_t* idx, const void* W, float* out, int32_t b, int32_t kk,

@@ -657,6 +657,10 @@ __device__ __forceinline__ void label_outer(const uint32_t (&pk)[K / 2], const f
     }
 }
 
+// v of another lane: a permutation within 16 lanes by the vector unit
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+
 // --------------------------------------------------------------------------------------------- the walk over the batch
 // Calls body(group, first LDS byte of its row, part) for every instance group of this part of the batch, with the rows staged
 // tile by tile; late(first group of the tile, groups in it, lane) right after a tile has arrived, early(first group,
