@@ -14,6 +14,12 @@ template <> __device__ __forceinline__ uint16_t stored<uint16_t>(float v) { retu
 typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
 template <typename TS> constexpr int VEC = 16 / (int)sizeof(TS);
+// ... as they lie in memory, in four registers
+template <typename TS> struct RawOf;
+template <> struct RawOf<float> { typedef f32x4 T; };
+template <> struct RawOf<uint16_t> { typedef u16x8 T; };
+__device__ __forceinline__ float value(const f32x4& q, int e) { return q[e]; }
+__device__ __forceinline__ float value(const u16x8& q, int e) { return usl_bf16_to_f32(q[e]); }
 
 __device__ __forceinline__ void load_vec(const float* p, float (&v)[4]) {
     const f32x4 q = *reinterpret_cast<const f32x4*>(p);
@@ -60,6 +66,8 @@ struct RowShare {
     __device__ __forceinline__ bool has_rest() const { return lane < rest; }
     template <typename T>
     __device__ __forceinline__ void load(const T* row, int g, float (&v)[V]) const { load_vec(row + min(at(g), whole - V), v); }
+    template <typename RAW, typename T>
+    __device__ __forceinline__ RAW load_raw(const T* row, int g) const { return *reinterpret_cast<const RAW*>(row + min(at(g), whole - V)); }
     template <typename T>
     __device__ __forceinline__ float load_rest(const T* row) const { return usl_to_f32(row[min(whole + lane, whole + rest - 1)]); }
 };
@@ -100,21 +108,22 @@ __device__ __forceinline__ T block_sum(T v, T* red) {
 // ---- forward: a row in the registers of LANES lanes, EPL values each (and one of the values behind the groups) --
 // Read once, written once.  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
 // around the row's mean, behind one barrier:  M2 = sum_w M2_w + n_w (mean_w - mean)^2.
-// FULL: there are both a weight and a bias.
-template <typename TS, int LANES, int EPL, bool FULL>
-__global__ void __launch_bounds__((LANES < 256 ? 256 : LANES))
+// FULL: there are both a weight and a bias; EARLY: they come with the row, not behind the sums.
+template <typename TS, int LANES, int EPL, bool FULL, bool EARLY>
+__global__ void __launch_bounds__((LANES < 256 ? 256 : LANES), (LANES == 1024 && EPL <= 32 && !EARLY ? 8 : 1))
 k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, TS* x /* may be h */, float* __restrict__ mean_out,
        float* __restrict__ rstd_out, int b, int d) {
     constexpr int V = VEC<TS>, G = EPL / V, NT = LANES < 256 ? 256 : LANES, WAVES = LANES / 64;
-    constexpr bool EARLY = FULL && EPL <= 16;   // weight and bias come with the row; more registers than that are not left
+    static_assert(FULL || !EARLY, "nothing to load early");
     int i = (int)blockIdx.x * (NT / LANES) + (int)threadIdx.x / LANES;
     if (LANES >= 64) i = __builtin_amdgcn_readfirstlane(i);
     if (i >= b) return;   // (rows of several wavefronts have a workgroup each)
     RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
-    float v[G][V], wg[EARLY ? G : 1][V], wb[EARLY ? G : 1][V];
+    typename RawOf<TS>::T v[G];
+    float wg[EARLY ? G : 1][V], wb[EARLY ? G : 1][V];
     const TS* from = h + (size_t)i * d;
 #pragma unroll
-    for (int g = 0; g < G; ++g) mine.load(from, g, v[g]);
+    for (int g = 0; g < G; ++g) v[g] = mine.template load_raw<typename RawOf<TS>::T>(from, g);
     float last = mine.load_rest(from);
     if (!mine.has_rest()) last = 0.f;
     if constexpr (EARLY) {
@@ -128,9 +137,9 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
     float s = last;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        float t = v[g][0];
+        float t = value(v[g], 0);
 #pragma unroll
-        for (int e = 1; e < V; ++e) t += v[g][e];
+        for (int e = 1; e < V; ++e) t += value(v[g], e);
         s += mine.has(g) ? t : 0.f;
     }
     int n = d;   // values of this wavefront
@@ -146,7 +155,7 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
     for (int g = 0; g < G; ++g) {
         float t = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) t = fmaf(v[g][e] - mean, v[g][e] - mean, t);
+        for (int e = 0; e < V; ++e) t = fmaf(value(v[g], e) - mean, value(v[g], e) - mean, t);
         m2 += mine.has(g) ? t : 0.f;
     }
     m2 = sum_lanes<LANES>(m2);
@@ -158,16 +167,11 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
             part[2][threadIdx.x >> 6] = (float)n;
         }
         __syncthreads();
-        float all = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) all = fmaf(part[0][w], part[2][w], all);
-        mean = all / (float)d;
-        m2 = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float off = part[0][w] - mean;
-            m2 += fmaf(part[2][w] * off, off, part[1][w]);
-        }
+        const int w = (int)threadIdx.x & 15;   // 16 lanes take a wavefront's each
+        const bool is = WAVES == 16 || w < WAVES;
+        const float mean_w = part[0][is ? w : 0], m2_w = is ? part[1][w] : 0.f, n_w = is ? part[2][w] : 0.f;
+        mean = sum16(mean_w * n_w) / (float)d;
+        m2 = sum16(fmaf(n_w * (mean_w - mean), mean_w - mean, m2_w));
     }
     const float rstd = 1.f / sqrtf(m2 / (float)d + eps);
     if (mine.lane == 0) {
@@ -189,7 +193,7 @@ k_norm(const TS* h, const float* __restrict__ gamma, const float* __restrict__ b
             if (FULL || beta) mine.load(beta, g, c);
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = fmaf((v[g][e] - mean) * rstd, w[e], c[e]);
+        for (int e = 0; e < V; ++e) o[e] = fmaf((value(v[g], e) - mean) * rstd, w[e], c[e]);
         if (mine.has(g)) store_vec(to + mine.at(g), o);
         if (!EARLY && g % 2) __builtin_amdgcn_sched_barrier(0);   // a few groups' weights at a time
     }
@@ -289,12 +293,10 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
                 part[turn][1][threadIdx.x >> 6] = sn;
             }
             __syncthreads();   // (two sets in turn: a set is written again behind the next barrier, which all reach behind their reads)
-            su = sn = 0.f;
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) {
-                su += part[turn][0][group * WAVES + q];
-                sn += part[turn][1][group * WAVES + q];
-            }
+            const int q = (int)threadIdx.x & 15;   // 16 lanes take a wavefront's each
+            const bool is = WAVES == 16 || q < WAVES;
+            su = sum16(is ? part[turn][0][group * WAVES + (is ? q : 0)] : 0.f);
+            sn = sum16(is ? part[turn][1][group * WAVES + (is ? q : 0)] : 0.f);
         }
         const float mu = su / (float)d, mn = sn / (float)d;
         mine.renew();
@@ -397,7 +399,7 @@ k_norm_grad_sums(const float* __restrict__ grad_x, const TS* __restrict__ h, con
 }
 
 // grad_h of a tile, and the tile's sums of grad_x n and grad_x over its rows into part[blockIdx.y][2][d].  A lane has 4 columns.  grid (columns, rows)
-constexpr int TILE_NT = 256, TILE_COLS = TILE_NT * 4, TILE_AT_ONCE = 4, TILE_ROWS = 2048 /* their statistics take 32 KB of LDS */;
+constexpr int TILE_NT = 256, TILE_COLS = TILE_NT * 4, TILE_AT_ONCE = 8, TILE_ROWS = 2048 /* their statistics take 32 KB of LDS */;
 __device__ __forceinline__ void load_four(const float* p, float (&v)[4]) { load_vec(p, v); }
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ void load_four(const uint16_t* p, float (&v)[4]) {
@@ -412,6 +414,31 @@ k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, con
                  int rows) {
     extern __shared__ __align__(16) float of_row[];   // [rows][4]: mean, rstd, mean of u, mean of u n
     const int i0 = (int)blockIdx.y * rows, n = min(rows, b - i0), lane = threadIdx.x & 63;
+    const int c = (int)blockIdx.x * TILE_COLS + (int)threadIdx.x * 4;
+    const bool full = (int)(blockIdx.x + 1) * TILE_COLS <= d;   // the same for the workgroup
+    float gx[2][TILE_AT_ONCE][4], v[2][TILE_AT_ONCE][4], w[4] = {1.f, 1.f, 1.f, 1.f}, sg[4] = {}, sb[4] = {};
+    // (loads without conditions, which the compiler would wait for: what is not there is another row's or column's)
+    auto load = [&](int r0, float (&g)[TILE_AT_ONCE][4], float (&x)[TILE_AT_ONCE][4]) {
+#pragma unroll
+        for (int a = 0; a < TILE_AT_ONCE; ++a) {
+            const size_t at = (size_t)(i0 + min(r0 + a, n - 1)) * d;
+            if (full) {
+                load_four(grad_x + at + c, g[a]);
+                load_four(h + at + c, x[a]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    g[a][e] = grad_x[at + min(c + e, d - 1)];
+                    x[a][e] = usl_to_f32(h[at + min(c + e, d - 1)]);
+                }
+            }
+        }
+    };
+    load(0, gx[0], v[0]);
+    if (gamma) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = gamma[min(c + e, d - 1)];
+    }
     for (int r = (int)(threadIdx.x >> 6); r < n; r += TILE_NT / 64) {
         float su = 0.f, sn = 0.f;
         for (int s = lane; s < splits; s += 64) {
@@ -429,38 +456,13 @@ k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, con
         }
     }
     __syncthreads();
-    const int c = (int)blockIdx.x * TILE_COLS + (int)threadIdx.x * 4;
-    if (c >= d) return;
-    const bool full = c + 4 <= d;
-    float w[4] = {1.f, 1.f, 1.f, 1.f}, sg[4] = {}, sb[4] = {};
-    if (gamma) {
-        if (full) load_vec(gamma + c, w);
-        else
-            for (int e = 0; e < 4; ++e) w[e] = c + e < d ? gamma[c + e] : 0.f;
-    }
     auto put = [&](float* to, const float (&o)[4]) {
         if (full) store_vec(to + c, o);
         else
             for (int e = 0; e < 4; ++e)
                 if (c + e < d) to[c + e] = o[e];
     };
-    for (int r0 = 0; r0 < n; r0 += TILE_AT_ONCE) {
-        float gx[TILE_AT_ONCE][4], v[TILE_AT_ONCE][4];
-#pragma unroll
-        for (int a = 0; a < TILE_AT_ONCE; ++a) {
-            const int r = min(r0 + a, n - 1);
-            const size_t at = (size_t)(i0 + r) * d;
-            if (full) {
-                load_four(grad_x + at + c, gx[a]);
-                load_four(h + at + c, v[a]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    gx[a][e] = c + e < d ? grad_x[at + c + e] : 0.f;
-                    v[a][e] = c + e < d ? usl_to_f32(h[at + c + e]) : 0.f;
-                }
-            }
-        }
+    auto work = [&](int r0, const float (&g)[TILE_AT_ONCE][4], const float (&x)[TILE_AT_ONCE][4]) {
 #pragma unroll
         for (int a = 0; a < TILE_AT_ONCE; ++a) {
             if (r0 + a >= n) break;
@@ -468,37 +470,60 @@ k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, con
             float o[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float u = gx[a][e] * w[e], m = (v[a][e] - k.x) * k.y;
+                const float u = g[a][e] * w[e], m = (x[a][e] - k.x) * k.y;
                 o[e] = k.y * (u - k.z - m * k.w);
-                sg[e] = fmaf(gx[a][e], m, sg[e]);
-                sb[e] += gx[a][e];
+                sg[e] = fmaf(g[a][e], m, sg[e]);
+                sb[e] += g[a][e];
             }
             put(grad_h + (size_t)(i0 + r0 + a) * d, o);
         }
+    };
+    // the next rows are asked for before these are written: the wait for a load is one for every store before it too
+    for (int r0 = 0; r0 < n; r0 += 2 * TILE_AT_ONCE) {
+        load(r0 + TILE_AT_ONCE, gx[1], v[1]);
+        work(r0, gx[0], v[0]);
+        load(r0 + 2 * TILE_AT_ONCE, gx[0], v[0]);
+        work(r0 + TILE_AT_ONCE, gx[1], v[1]);
     }
     if (!part) return;
     put(part + ((size_t)blockIdx.y * 2) * d, sg);
     put(part + ((size_t)blockIdx.y * 2 + 1) * d, sb);
 }
 
-// The parts' sums, added up in a fixed order: 64 columns of [2][d] a workgroup, a sixteenth of the parts a wavefront.
-__global__ void __launch_bounds__(1024)
+// The parts' sums, added up in a fixed order: a lane takes COLS columns of one of the two sums and every GROUPS-th part, the groups join through LDS.
+template <int COLS, int GROUPS>
+__global__ void __launch_bounds__(64 * GROUPS)
 k_norm_sum_parts(const float* __restrict__ part, int parts, int d, float* __restrict__ grad_gamma, float* __restrict__ grad_beta) {
-    __shared__ float red[16][64];
-    const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+    constexpr int AT_ONCE = 8;
+    __shared__ float red[GROUPS][64 * COLS];
+    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6, c = ((int)blockIdx.x * 64 + lane) * COLS;
     float* to = blockIdx.y ? grad_beta : grad_gamma;
     if (!to) return;
-    float s = 0.f;
-    if (col < d) {
-#pragma unroll 4
-        for (int p = wave; p < parts; p += 16) s += part[((size_t)p * 2 + blockIdx.y) * d + col];
-    }
-    red[wave][threadIdx.x & 63] = s;
-    __syncthreads();
-    if (wave || col >= d) return;
+    float s[COLS] = {};
+    const float* from = part + (size_t)blockIdx.y * d;
+    const int first = min(c, d - COLS);   // (the last lanes take the last columns: the same sums as another lane's)
+    for (int p0 = group; p0 < parts; p0 += AT_ONCE * GROUPS) {
+        float v[AT_ONCE][COLS];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += red[w][threadIdx.x];
-    to[col] = s;
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const float* at = from + (size_t)min(p0 + u * GROUPS, parts - 1) * 2 * d + first;
+            if constexpr (COLS == 4) load_vec(at, v[u]);
+            else v[u][0] = *at;
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int e = 0; e < COLS; ++e) s[e] += p0 + u * GROUPS < parts ? v[u][e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) red[group][lane * COLS + e] = s[e];
+    __syncthreads();
+    for (int q = threadIdx.x; q < 64 * COLS; q += 64 * GROUPS) {
+        float t = red[0][q];
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g) t += red[g][q];
+        to[min((int)blockIdx.x * 64 * COLS + q / COLS * COLS, d - COLS) + q % COLS] = t;
+    }
 }
 
 }  // namespace
@@ -507,9 +532,14 @@ k_norm_sum_parts(const float* __restrict__ part, int parts, int d, float* __rest
 // workgroup have 32 or 64 values a lane.
 template <typename TS>
 static usl_status norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b) {
-#define USL_NORM(LANES, EPL) do { if (gamma && beta) USL_NORM_F(LANES, EPL, true); else USL_NORM_F(LANES, EPL, false); } while (0)
-#define USL_NORM_F(LANES, EPL, FULL)                                                                                                \
-    hipLaunchKernelGGL((k_norm<TS, LANES, EPL, FULL>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
+#define USL_NORM(LANES, EPL)                                                                         \
+    do {                                                                                             \
+        if (!gamma || !beta) USL_NORM_F(LANES, EPL, false, false);                                   \
+        else if (EPL <= 16 || (EPL == 32 && b <= c->num_cu)) USL_NORM_F(LANES, EPL, true, (EPL <= 32)); \
+        else USL_NORM_F(LANES, EPL, true, false);                                                    \
+    } while (0)
+#define USL_NORM_F(LANES, EPL, FULL, EARLY)                                                                                         \
+    hipLaunchKernelGGL((k_norm<TS, LANES, EPL, FULL, EARLY>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
                        dim3(LANES < 256 ? 256 : LANES), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, b, c->d)
 #define USL_NORM_ANY hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d)
     if (c->d < VEC<TS>) USL_NORM_ANY;
@@ -606,7 +636,11 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
         USL_TRY(usl_check_launch(c, "layer_norm_backward"));
         if (!sums) return USL_OK;
     }
-    hipLaunchKernelGGL(k_norm_sum_parts, dim3((unsigned)((d + 63) / 64), 2), dim3(1024), 0, c->stream, c->norm_part, s.parts, d, grad_gamma, grad_beta);
+    // few sets of long sums, or many of short ones
+    if (s.parts <= 32 && d >= 4)
+        hipLaunchKernelGGL((k_norm_sum_parts<4, 4>), dim3((unsigned)((d + 255) / 256), 2), dim3(256), 0, c->stream, c->norm_part, s.parts, d, grad_gamma, grad_beta);
+    else
+        hipLaunchKernelGGL((k_norm_sum_parts<1, 16>), dim3((unsigned)((d + 63) / 64), 2), dim3(1024), 0, c->stream, c->norm_part, s.parts, d, grad_gamma, grad_beta);
     return usl_check_launch(c, "layer_norm_backward");
 }
 
