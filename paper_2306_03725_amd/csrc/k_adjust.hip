@@ -14,7 +14,7 @@ constexpr int AD_NT = 256;
 // scores a lane holds: 16, or 8 where that would leave most of the chip without a workgroup.  (32 of them, with 32 KB of counts and 124 registers, leave a
 // compute unit three workgroups: 256 x 500k scores written in 241 us, with 16 in 210.)
 constexpr int AD_EPT = 16, AD_EPT_FEW = 8;
-constexpr int RUN_WORKGROUPS = 8;   // of k_topk_adjusted, to a compute unit
+constexpr int RUN_WORKGROUPS = 4;   // of k_topk_adjusted, to a compute unit: as many as it holds; a run pays for its first threshold (256 x 670k, 10 labels: 162 us, with 8 171, with 16 197)
 
 typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));   // rows and segments begin at any float
 
@@ -275,6 +275,28 @@ k_topk_adjusted(const float* __restrict__ out, int64_t m, Adjust a, int kk, int 
     for (int r = tid; r < kk; r += AD_NT) to[r] = list[r];
 }
 
+// ... of one segment an instance's run has, where that many workgroups are few: every lane's scores become keys, and no threshold is worth its maxima.
+template <int EPT, bool BIAS, bool MASK>
+__global__ void __launch_bounds__(AD_NT)
+k_topk_adjusted_few(const float* __restrict__ out, int64_t m, Adjust a, int kk, uint64_t* __restrict__ cand) {
+    __shared__ __align__(16) uint32_t counts[AD_NT * EPT];
+    __shared__ uint64_t list[AD_NT / 64 * TOPK_MAX];
+    const int64_t seg0 = (int64_t)blockIdx.x * (AD_NT * EPT);
+    const int lim = (int)min((int64_t)AD_NT * EPT, m - seg0);
+    Segment<EPT, BIAS, MASK> seg;
+    float bias[EPT];
+    seg.load(out + (int64_t)blockIdx.y * m, seg0, lim, (int)blockIdx.y, a);
+    seg.load_bias(seg0, lim, a, bias);
+    const Shown shown(a, (int)blockIdx.y);
+    if (shown.any()) clear<EPT>(counts);
+    seg.adjust(shown, seg0, lim, a, bias, counts, __uint_as_float(0x7FC00000u));
+    uint64_t held[EPT];
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) held[e] = seg.v[e] == seg.v[e] ? score_key(seg.v[e], (uint32_t)(seg0 + local_label(e))) : 0ull;   // (NaN: not to be given)
+    const uint64_t own = best_keys<AD_NT / 64>(held, kk, list);
+    if ((int)threadIdx.x < kk) cand[((size_t)blockIdx.y * gridDim.x + blockIdx.x) * kk + threadIdx.x] = own;
+}
+
 Adjust of(const usl_ctx* c, const usl_adjustments* a) {
     const int64_t words = (c->m + 31) / 32;
     return Adjust{a->bias, a->allowed, a->allowed_rows == 1 ? 0 : words, a->shown_off, a->shown_lab, a->repeat, a->presence, a->frequency};
@@ -295,11 +317,7 @@ size_t usl_adjusted_segments(const usl_ctx* c) {   // b * runs_of(.., b), for an
     return most > most_few ? most : most_few;
 }
 
-// the kernel by what there is to do and how much of it
-#define USL_ADJUST_BY(RUN)                                                                    \
-    do {                                                                                      \
-        if (few) USL_ADJUST_BY_WHAT(RUN, AD_EPT_FEW); else USL_ADJUST_BY_WHAT(RUN, AD_EPT);   \
-    } while (0)
+// the kernel by what there is to do
 #define USL_ADJUST_BY_WHAT(RUN, EPT)                                                          \
     do {                                                                                      \
         if (a->bias) { if (a->allowed) RUN(EPT, true, true); else RUN(EPT, true, false); }    \
@@ -310,7 +328,8 @@ usl_status usl_launch_adjust(usl_ctx* c, const float* out, const usl_adjustments
     const bool few = few_segments(c, b);
     const dim3 grid((unsigned)segments(c, few ? AD_EPT_FEW : AD_EPT), (unsigned)b);
 #define USL_ADJUST(EPT, BIAS, MASK) hipLaunchKernelGGL((k_adjust<EPT, BIAS, MASK>), grid, dim3(AD_NT), 0, c->stream, out, c->m, of(c, a), adjusted)
-    USL_ADJUST_BY(USL_ADJUST);
+    if (few) USL_ADJUST_BY_WHAT(USL_ADJUST, AD_EPT_FEW);
+    else USL_ADJUST_BY_WHAT(USL_ADJUST, AD_EPT);
 #undef USL_ADJUST
     return usl_check_launch(c, "adjust_scores");
 }
@@ -320,9 +339,13 @@ usl_status usl_launch_topk_adjusted(usl_ctx* c, const float* out, const usl_adju
     const int nseg = segments(c, few ? AD_EPT_FEW : AD_EPT), runs = few ? nseg : runs_of(c, nseg, b);
     USL_TRY(usl_reserve_topk(c));
     const dim3 grid((unsigned)runs, (unsigned)b);
+#define USL_BEST_FEW(EPT, BIAS, MASK) \
+    hipLaunchKernelGGL((k_topk_adjusted_few<EPT, BIAS, MASK>), grid, dim3(AD_NT), 0, c->stream, out, c->m, of(c, a), (int)kk, c->topk_cand)
 #define USL_BEST(EPT, BIAS, MASK) \
     hipLaunchKernelGGL((k_topk_adjusted<EPT, BIAS, MASK>), grid, dim3(AD_NT), 0, c->stream, out, c->m, of(c, a), (int)kk, nseg, c->topk_cand)
-    USL_ADJUST_BY(USL_BEST);
+    if (few) USL_ADJUST_BY_WHAT(USL_BEST_FEW, AD_EPT_FEW);
+    else USL_ADJUST_BY_WHAT(USL_BEST, AD_EPT);
 #undef USL_BEST
+#undef USL_BEST_FEW
     return usl_launch_topk_merge(c, runs, b, kk, top_lab, top_val);
 }

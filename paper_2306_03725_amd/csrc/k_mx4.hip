@@ -14,14 +14,17 @@ __device__ __forceinline__ uint32_t mx4_scale_byte(uint32_t amax) {
 // A lane takes four neighbouring slots of a label; the lanes of a block of 32 slots are neighbours, 8 of them (1, 2 or 4 where a label has 16 slots or
 // fewer), so their largest magnitude is found by lane permutations, and two lanes make a word.  ITEMS such pieces of a lane are on their way together.
 // Bound by the stream of the values.
-constexpr int ITEMS = 4;
+#ifndef IT
+#define IT 2
+#endif
+constexpr int ITEMS = IT;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));        // a row of k values begins at any of them
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
 
 int lanes_of_label(int k) { return k <= 4 ? 1 : k <= 8 ? 2 : k <= 16 ? 4 : mx4_blocks(k) * 8; }
 
-// Piece `item` of this lane: label and first slot (label m: none)
+// Piece `item` of this lane: label (m: none) and first slot
 struct Pieces {
     int64_t j0, m;
     uint32_t rest, per;   // the workgroup's first piece is number `rest` of label j0; pieces of a label
@@ -44,8 +47,9 @@ __device__ __forceinline__ uint32_t max_of_pair(uint32_t v) {
     return t > v ? t : v;
 }
 
-// G: lanes of a block
-template <typename TS, int G>
+// G: lanes of a block; FOURS: k is a multiple of 4.  Loads have no conditions, which the compiler would wait for: a lane whose piece does not exist loads
+// another one, and makes nothing of it.
+template <typename TS, int G, bool FOURS>
 __global__ void __launch_bounds__(256)
 k_mx4_quantize(const TS* __restrict__ W, uint32_t* __restrict__ codes, uint8_t* __restrict__ scales, int64_t m, int k, int per) {
     const Pieces pieces(m, per);
@@ -54,21 +58,26 @@ k_mx4_quantize(const TS* __restrict__ W, uint32_t* __restrict__ codes, uint8_t* 
     int slot[ITEMS];
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
-        const int64_t j = label[u] = pieces.label(u, &slot[u]);
-        const int t = slot[u];
-        const TS* from = W + (size_t)j * k + t;
-        if (j < m && t + 4 <= k) {
-            if constexpr (sizeof(TS) == 4) {
-                const f32x4 q = *reinterpret_cast<const f32x4*>(from);
-                v[u][0] = q.x; v[u][1] = q.y; v[u][2] = q.z; v[u][3] = q.w;
-            } else {
-                const u16x4 q = *reinterpret_cast<const u16x4*>(from);
-                v[u][0] = usl_bf16_to_f32(q.x); v[u][1] = usl_bf16_to_f32(q.y); v[u][2] = usl_bf16_to_f32(q.z); v[u][3] = usl_bf16_to_f32(q.w);
-            }
+        label[u] = pieces.label(u, &slot[u]);
+        const TS* row = W + (size_t)min(label[u], m - 1) * k;
+        if constexpr (FOURS && sizeof(TS) == 4) {
+            const f32x4 q = *reinterpret_cast<const f32x4*>(row + min(slot[u], k - 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = q[e];
+        } else if constexpr (FOURS) {
+            const u16x4 q = *reinterpret_cast<const u16x4*>(row + min(slot[u], k - 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = usl_bf16_to_f32(q[e]);
         } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[u][q] = j < m && t + q < k ? usl_to_f32(from[q]) : 0.f;
+            for (int e = 0; e < 4; ++e) v[u][e] = usl_to_f32(row[min(slot[u] + e, k - 1)]);
         }
+    }
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (slot[u] + (FOURS ? 0 : e) >= k) v[u][e] = 0.f;
     }
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
@@ -101,10 +110,10 @@ k_mx4_dequantize(const uint32_t* __restrict__ codes, const uint8_t* __restrict__
     int slot[ITEMS];
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
-        const int64_t j = label[u] = pieces.label(u, &slot[u]);
-        const bool in = j < m && slot[u] < k;
-        word[u] = in ? codes[j * mx4_words(k) + (slot[u] >> 3)] : 0u;
-        byte[u] = in ? scales[j * mx4_blocks(k) + slot[u] / MX4_BLOCK] : 0u;
+        label[u] = pieces.label(u, &slot[u]);
+        const int64_t j = min(label[u], m - 1);
+        word[u] = codes[j * mx4_words(k) + min(slot[u] >> 3, mx4_words(k) - 1)];
+        byte[u] = scales[j * mx4_blocks(k) + min(slot[u] / MX4_BLOCK, mx4_blocks(k) - 1)];
     }
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
@@ -163,7 +172,8 @@ k_mx4_forward_any(const TS* __restrict__ x, const int32_t* __restrict__ idx, con
 usl_status usl_launch_mx4_quantize(usl_ctx* c, const void* W, uint32_t* codes, uint8_t* scales) {
     const int per = lanes_of_label(c->k);
     const unsigned n = (unsigned)((c->m * per + 256 * ITEMS - 1) / (256 * ITEMS));
-#define USL_QUANTIZE(TS, G) hipLaunchKernelGGL((k_mx4_quantize<TS, G>), dim3(n), dim3(256), 0, c->stream, (const TS*)W, codes, scales, c->m, c->k, per)
+#define USL_QUANTIZE_F(TS, G, FOURS) hipLaunchKernelGGL((k_mx4_quantize<TS, G, FOURS>), dim3(n), dim3(256), 0, c->stream, (const TS*)W, codes, scales, c->m, c->k, per)
+#define USL_QUANTIZE(TS, G) do { if (c->k % 4 == 0) USL_QUANTIZE_F(TS, G, true); else USL_QUANTIZE_F(TS, G, false); } while (0)
 #define USL_QUANTIZE_G(TS)                       \
     do {                                         \
         if (per == 1) USL_QUANTIZE(TS, 1);       \
@@ -175,6 +185,7 @@ usl_status usl_launch_mx4_quantize(usl_ctx* c, const void* W, uint32_t* codes, u
     else USL_QUANTIZE_G(uint16_t);
 #undef USL_QUANTIZE_G
 #undef USL_QUANTIZE
+#undef USL_QUANTIZE_F
     return usl_check_launch(c, "quantize_mx4");
 }
 

@@ -81,6 +81,45 @@ k_topk_merge(const uint64_t* __restrict__ cand, int n, int kk, int32_t* __restri
     }
 }
 
+// Rows of few candidates, a wavefront each: no barriers.  (256 rows of 80, 10 labels: 8.1 us by a workgroup each and barriers, 4.8 so.)
+constexpr int MERGE_HELD = 4;
+__global__ void __launch_bounds__(256)
+k_topk_merge_few(const uint64_t* __restrict__ cand, int n, int b, int kk, int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
+    const int i = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (i >= b) return;
+    const uint64_t* c = cand + (size_t)i * n;
+    uint64_t mine[MERGE_HELD];
+#pragma unroll
+    for (int q = 0; q < MERGE_HELD; ++q) {
+        const uint64_t key = c[min(q * 64 + lane, n - 1)];
+        mine[q] = q * 64 + lane < n ? key : 0ull;
+    }
+    const uint64_t best = best_keys<1>(mine, kk, nullptr);
+    if (lane >= kk) return;
+    top_lab[(size_t)i * kk + lane] = best ? key_label(best) : -1;
+    top_val[(size_t)i * kk + lane] = best ? key_score(best) : -INFINITY;
+}
+
+// Rows of more, a workgroup each: its wavefronts find theirs, the first one the row's.  (1225 candidates, 5 labels: 4.1 us with a barrier a label, 3.6 so;
+// 256 rows of 410: 8.2 and 6.5; 7840, 32 labels: 56 and 32.)
+constexpr int MERGE_ROW_HELD = 8, MERGE_LONG_HELD = 16;
+template <int NT, int HELD>
+__global__ void __launch_bounds__(NT)
+k_topk_merge_row(const uint64_t* __restrict__ cand, int n, int kk, int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
+    __shared__ uint64_t list[NT / 64 * TOPK_MAX];
+    const uint64_t* c = cand + (size_t)blockIdx.x * n;
+    uint64_t mine[HELD];
+#pragma unroll
+    for (int q = 0; q < HELD; ++q) {
+        const uint64_t key = c[min(q * NT + (int)threadIdx.x, n - 1)];
+        mine[q] = q * NT + (int)threadIdx.x < n ? key : 0ull;
+    }
+    const uint64_t best = best_keys<NT / 64>(mine, kk, list);
+    if ((int)threadIdx.x >= kk) return;
+    top_lab[(size_t)blockIdx.x * kk + threadIdx.x] = best ? key_label(best) : -1;
+    top_val[(size_t)blockIdx.x * kk + threadIdx.x] = best ? key_score(best) : -INFINITY;
+}
+
 __global__ void k_zero_hits(unsigned long long* hits, int kk) {
     if ((int)threadIdx.x < kk) hits[threadIdx.x] = 0ull;
 }
@@ -132,8 +171,12 @@ usl_status usl_reserve_topk(usl_ctx* c) {
 // The best kk of every row from nseg sets of kk candidates each (usl_ctx::topk_cand).
 usl_status usl_launch_topk_merge(usl_ctx* c, int nseg, int32_t b, int32_t kk, int32_t* top_lab, float* top_val) {
     const int n = nseg * kk;
-    if (n <= TOPK_SHORT_MERGE)
-        hipLaunchKernelGGL(k_topk_merge<TK_NT>, dim3((unsigned)b), dim3(TK_NT), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
+    if (n <= MERGE_HELD * 64)
+        hipLaunchKernelGGL(k_topk_merge_few, dim3((unsigned)((b + 3) / 4)), dim3(256), 0, c->stream, c->topk_cand, n, (int)b, (int)kk, top_lab, top_val);
+    else if (n <= MERGE_ROW_HELD * 256)
+        hipLaunchKernelGGL((k_topk_merge_row<256, MERGE_ROW_HELD>), dim3((unsigned)b), dim3(256), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
+    else if (n <= MERGE_LONG_HELD * 1024)
+        hipLaunchKernelGGL((k_topk_merge_row<1024, MERGE_LONG_HELD>), dim3((unsigned)b), dim3(1024), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
     else
         hipLaunchKernelGGL(k_topk_merge<1024>, dim3((unsigned)b), dim3(1024), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
     return usl_check_launch(c, "topk");

@@ -73,6 +73,30 @@ struct BlockMax {
     }
 };
 
+// The kk largest of the keys that the lanes of WAVES wavefronts hold (0: none), the r-th in lane r of wavefront 0 (0 where there are no more): every wavefront
+// its own, without a barrier, then the first one all of theirs.  list: WAVES * kk places.
+template <int WAVES, int HELD>
+__device__ __forceinline__ uint64_t best_keys(const uint64_t (&held)[HELD], int kk, uint64_t* list) {
+    const int lane = threadIdx.x & 63;
+    uint64_t prev = ~0ull, found = 0;
+    for (int r = 0; r < kk; ++r) {
+        uint64_t best = 0;
+#pragma unroll
+        for (int q = 0; q < HELD; ++q)
+            if (held[q] < prev && held[q] > best) best = held[q];
+        prev = wave_max(best);
+        found = lane == r ? prev : found;
+    }
+    if (WAVES == 1) return found;
+    if (lane < kk) list[(threadIdx.x >> 6) * kk + lane] = found;
+    __syncthreads();
+    if (threadIdx.x >= 64) return 0;
+    uint64_t mine[(WAVES * TOPK_MAX + 63) / 64];
+#pragma unroll
+    for (int q = 0; q < (WAVES * TOPK_MAX + 63) / 64; ++q) mine[q] = q * 64 + lane < WAVES * kk ? list[q * 64 + lane] : 0ull;
+    return best_keys<1>(mine, kk, list);
+}
+
 template <int NT>
 struct TopkSegment {
     uint64_t red[2][NT / 64];
