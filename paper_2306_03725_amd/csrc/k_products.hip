@@ -637,7 +637,7 @@ Launch choose(const usl_ctx* c, const Layout& L, int b, ProductKind kind, int mo
         const double t_even = clocks(kern, best.geom, res, n * best.G, gpb, labels) + sums_of(best.G);
         return t_even * (with_loss && kern.NT == 256 ? 1.2 : 1.1) < t ? labels : 0;
     };
-    for (int shape = 0; shape < 4; ++shape) {
+    for (int shape = 0; shape < 6; ++shape) {   // (4 and 5: values in 4 bits only)
         if (shape_force >= 0 && shape != shape_force && kernel_for(c, L, kind, shape_force).fn) continue;
         const ProductKernel kern = kernel_for(c, L, kind, shape);
         if (!kern.fn) continue;

@@ -452,6 +452,21 @@ struct Mx4Row {
         wave_sync();
         return mine;
     }
+    // ... or as codes, eight to a register, which a label of one block leaves in place (their scale is the sum's)
+    __device__ __forceinline__ void unpack(uint32_t* lds, const SlotOrder<K>& so, int k, uint32_t (&c)[K / 8]) const {
+        const uint32_t* mine = put(lds);
+#pragma unroll
+        for (int q = 0; q < K / 8; ++q) {
+            c[q] = 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int slot = so.at(8 * q + u);
+                c[q] |= slot < k ? (mine[slot >> 3] >> (4 * (slot & 7)) & 15u) << (4 * u) : 0u;
+            }
+            asm volatile("" : "+v"(c[q]));   // here, not where it is first used: eight registers instead of one until then
+        }
+        wave_sync();
+    }
     __device__ __forceinline__ void unpack(uint32_t* lds, const SlotOrder<K>& so, int k, float (&w)[K]) const {
         const uint32_t* mine = put(lds);
 #pragma unroll
@@ -625,6 +640,50 @@ __device__ __forceinline__ void label_dot(const uint32_t (&pk)[K / 2], const uin
     }
 }
 
+// Codes of values in 4 bits, eight to a register: one instruction makes the weights of two steps of them.
+template <int K, typename TS, int Q, bool HALVES>
+__device__ __forceinline__ void label_dot_mx4(const uint32_t (&pk)[K / 2], const uint32_t (&c)[K / 8], uint32_t base, uint32_t zbyte, float (&acc)[Q]) {
+    constexpr int B = sizeof(TS) == 4 ? batch_of<float, Q>() : 8;
+    typedef typename Unit<TS, Q>::T U;
+#pragma unroll
+    for (int t0 = 0; t0 < K; t0 += B) {
+        U v[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) v[u] = gather<TS, Q, HALVES>(pk, t0 + u, base, zbyte);
+#pragma unroll
+        for (int u = 0; u < B; u += 2) {
+            const uint32_t word = c[(t0 + u) / 8];
+            const int byte = (t0 + u) % 8 / 2;
+            if constexpr (sizeof(TS) == 4) {
+                const f32x2 w = byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 1)
+                              : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 3);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if constexpr (Q == 1) acc[0] = fmaf(w[s], v[u + s], acc[0]);
+                    else {
+#pragma unroll
+                        for (int q = 0; q < Q; ++q) acc[q] = fmaf(w[s], v[u + s][q], acc[q]);
+                    }
+                }
+            } else {
+                const uint32_t w2 = __builtin_bit_cast(uint32_t, byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 1)
+                                                               : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 2) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 3));
+                if constexpr (Q == 1) acc[0] = dot2((uint32_t)v[u] | ((uint32_t)v[u + 1] << 16), w2, acc[0]);
+                else if constexpr (Q == 2) {
+                    acc[0] = dot2(join_lo(v[u], v[u + 1]), w2, acc[0]);
+                    acc[1] = dot2(join_hi(v[u], v[u + 1]), w2, acc[1]);
+                } else {
+                    acc[0] = dot2(join_lo(v[u].x, v[u + 1].x), w2, acc[0]);
+                    acc[1] = dot2(join_hi(v[u].x, v[u + 1].x), w2, acc[1]);
+                    acc[2] = dot2(join_lo(v[u].y, v[u + 1].y), w2, acc[2]);
+                    acc[3] = dot2(join_hi(v[u].y, v[u + 1].y), w2, acc[3]);
+                }
+            }
+        }
+        schedule_batch<HALVES, B, B * Q + B / 2>();
+    }
+}
+
 // acc[s] += sum over the group's instances of g[q] * x[instance q]
 template <int K, typename TS, int Q, bool HALVES>
 __device__ __forceinline__ void label_outer(const uint32_t (&pk)[K / 2], const float (&gv)[Q], uint32_t base, uint32_t zbyte, float (&acc)[K]) {
@@ -726,6 +785,9 @@ __device__ __forceinline__ void walk(const char* __restrict__ xi, uint32_t lds0,
 template <typename TS, int K> struct WReg;                      // weights of one label in registers
 template <int K> struct WReg<float, K> { float v[K]; };
 template <int K> struct WReg<uint16_t, K> { uint32_t v[K / 2]; };
+template <int K> struct WCodes { uint32_t v[K / 8]; float scale; };   // ... as codes of one block
+// Labels of one block keep their codes: 4 bits a slot where float32 takes 32, so a lane has twice the labels, and half the workgroups copy the rows.
+template <int K, bool MX4> constexpr bool keeps_codes() { return MX4 && K <= 32; }
 
 __device__ __forceinline__ uint32_t lds_base(const void* p) {
     return (uint32_t)(uintptr_t)((const __attribute__((address_space(3))) void*)p);
@@ -770,7 +832,8 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
         if (threadIdx.x < (n & 3)) to[(n & ~(size_t)3) + threadIdx.x] = 0.f;
     }
     uint32_t pk[LPT][K / 2];
-    WReg<TS, K> w[LPT];
+    constexpr bool CODES = keeps_codes<K, MX4>();
+    typename std::conditional<CODES, WCodes<K>, WReg<TS, K>>::type w[LPT];
 #pragma unroll
     for (int l = 0; l < LPT; ++l) {
         const int64_t row0 = j0 + (int64_t)l * NT;
@@ -778,7 +841,7 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
             Mx4Row<K> row;
             row.load(reinterpret_cast<const uint32_t*>(W), scales, row0 + threadIdx.x, row0 + threadIdx.x < end, k);
             SlotOrder<K> so;
-            if constexpr (raw_rows<TS, K, NT>()) {
+            if constexpr (raw_rows<TS, K, NT>() && !CODES) {
                 RawRows<TS, K> raw;
                 raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
                 unpack_idx<K, TS>(raw, k, reinterpret_cast<uint32_t*>(lds_raw), pk[l]);
@@ -787,7 +850,12 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 so.load(perm, row0 + threadIdx.x, row0 + threadIdx.x < end);
                 fetch_idx<K>(idx, row0, end, k, (uint32_t)tg.zero_col, reinterpret_cast<uint32_t*>(lds_raw), so, pk[l]);
             }
+            if constexpr (CODES) keep_packed(pk[l]);
             row.unpack(reinterpret_cast<uint32_t*>(lds_raw), so, k, w[l].v);
+            if constexpr (CODES) {
+                w[l].scale = row.scale[0];
+                __builtin_amdgcn_sched_barrier(0);   // one label after the other: several at a time would not fit beside those that are resident
+            }
         } else if constexpr (raw_rows<TS, K, NT>()) {
             RawRows<TS, K> raw;
             raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
@@ -870,6 +938,7 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 for (int q = 0; q < Q; ++q)
                     if (g * Q + q < b) {
                         float o = z[q];
+                        if constexpr (CODES) o *= w[l].scale;
                         if (LOSS) {
                             const usl_loss_parts r = usl_loss_in_parts(LOSS == 2 ? 1 : loss.kind, o, any_target.value && (hits >> q & 1u) ? 1.f : 0.f, loss.scale);
                             o = r.g;
@@ -911,7 +980,11 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 for (int q = 0; q < Q; ++q) acc[q] = HALVES && part ? prev[DELAY ? l : 0][q] : 0.f;   // the first half's sums
                 keep_packed(pk[l]);
                 __builtin_amdgcn_s_setprio(1);
-                if (!EVEN || wave0 + l * NT < nlab) label_dot<K, Q, HALVES>(pk[l], w[l].v, base, zbyte, acc);
+                if constexpr (CODES) keep_packed(w[l].v);
+                if (!EVEN || wave0 + l * NT < nlab) {
+                    if constexpr (CODES) label_dot_mx4<K, TS, Q, HALVES>(pk[l], w[l].v, base, zbyte, acc);
+                    else label_dot<K, Q, HALVES>(pk[l], w[l].v, base, zbyte, acc);
+                }
                 __builtin_amdgcn_s_setprio(0);
                 // finish the sums here; left alone the compiler sinks the multiply-adds into the guarded store
                 // and keeps every gathered value alive until then
