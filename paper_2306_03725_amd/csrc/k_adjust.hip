@@ -306,15 +306,21 @@ bool few_segments(const usl_ctx* c, int32_t b) { return (int64_t)segments(c, AD_
 
 }  // namespace
 
-// Runs of an instance's segments: as many as give every compute unit RUN_WORKGROUPS workgroups.
-static int runs_of(const usl_ctx* c, int nseg, int32_t b) {
-    const int64_t want = ((int64_t)c->num_cu * RUN_WORKGROUPS + b - 1) / b;
-    return (int)(want < nseg ? want : nseg);
+// Best labels: a workgroup for every short segment, or runs of segments under one threshold?  A run pays for its thresholds' maxima and waits out its segments one
+// after the other; a segment by itself pays for its lanes' keys, the more the more labels are asked for.  us, by segments and by runs: 20k x 64, 5 labels (640 short
+// segments) 10.4 and 15.9; 41k x 173 (3460) 19.3 and 22.5; 46k x 92, 1 label (2116) 10.6 and 15.8; 58k x 49, 10 labels (1421) 18.4 and 20.2; not so 100k x 100, 5 labels
+// (4900) 24.3 and 25.1; 58k x 49, 32 labels 43.4 and 37.9; 41k x 600, 5 labels (12 000) 48.4 and 43.4; 747k x 57 79.1 and 50.3.
+static bool best_by_segments(const usl_ctx* c, int32_t b, int32_t kk) { return (int64_t)segments(c, AD_EPT_FEW) * b * (kk + 5) <= 35000 / 256 * (int64_t)c->num_cu; }
+// Runs of an instance's segments: no more than the chip holds together (one more workgroup takes as long as another round of them: 747k x 57 50.3 us with 17 runs, 104.6 with
+// 18), and eight labels asked for are worth a segment of a run (100k x 100, 32 labels: 46.9 us with 5 runs, 55.7 with 10).
+static int runs_of(const usl_ctx* c, int nseg, int32_t b, int32_t kk) {
+    const int64_t room = (int64_t)c->num_cu * RUN_WORKGROUPS / b, most = kk > 8 ? nseg / (kk / 8) : nseg, runs = room < most ? room : most;
+    return runs < 1 ? 1 : (int)runs;
 }
 
-size_t usl_adjusted_segments(const usl_ctx* c) {   // b * runs_of(.., b), for any b up to max_b
-    const size_t most = (size_t)c->num_cu * RUN_WORKGROUPS + c->max_b, most_few = (size_t)segments(c, AD_EPT_FEW) * (c->num_cu / segments(c, AD_EPT) + 1);
-    return most > most_few ? most : most_few;
+size_t usl_adjusted_segments(const usl_ctx* c) {   // b * sets of candidates an instance has, for any b up to max_b
+    const size_t by_runs = (size_t)c->num_cu * RUN_WORKGROUPS + c->max_b, by_segments = (size_t)(35000 / 256 * (int64_t)c->num_cu / 6) + 1;
+    return by_runs > by_segments ? by_runs : by_segments;
 }
 
 // the kernel by what there is to do
@@ -335,8 +341,8 @@ usl_status usl_launch_adjust(usl_ctx* c, const float* out, const usl_adjustments
 }
 
 usl_status usl_launch_topk_adjusted(usl_ctx* c, const float* out, const usl_adjustments* a, int32_t b, int32_t kk, int32_t* top_lab, float* top_val) {
-    const bool few = few_segments(c, b);
-    const int nseg = segments(c, few ? AD_EPT_FEW : AD_EPT), runs = few ? nseg : runs_of(c, nseg, b);
+    const bool few = best_by_segments(c, b, kk);
+    const int nseg = segments(c, few ? AD_EPT_FEW : AD_EPT), runs = few ? nseg : runs_of(c, nseg, b, kk);
     USL_TRY(usl_reserve_topk(c));
     const dim3 grid((unsigned)runs, (unsigned)b);
 #define USL_BEST_FEW(EPT, BIAS, MASK) \

@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(BWD_NT)
 k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
             const float* __restrict__ rstd_in, float* __restrict__ grad_h, float* __restrict__ to_gamma, float* __restrict__ to_beta, size_t stride, int b, int d) {
     constexpr int V = VEC<TS>, G = EPL / V, ROWS = BWD_NT / LANES, WAVES = LANES / 64;
-    extern __shared__ __align__(16) float lds[];   // [ROWS][2][EPL + 1][LANES], with one row none
+    extern __shared__ __align__(16) float lds[];   // [row groups, or up to 4 those but the first][2][EPL + 1][LANES]
     __shared__ float part[2][2][BWD_NT / 64];
     RowShare<LANES, V> mine((int)threadIdx.x % LANES, d);
     int group = (int)threadIdx.x / LANES;
@@ -310,7 +310,35 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
         if (in && mine.has_rest()) grad_h[at + mine.whole + mine.lane] = rstd * (last_g - mu - last_n * mn);
     }
     if (!to_gamma && !to_beta) return;
-    if constexpr (ROWS == 1) {
+    if constexpr (ROWS <= 4) {   // long rows: the first group joins the others' sums to its own
+        constexpr int E = EPL + 1, ENTRIES = 2 * E * LANES;   // [2][value of a lane, the rest][lane]
+        if (ROWS > 1 && group > 0) {
+            float* own = lds + (group - 1) * ENTRIES + mine.lane;
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    own[(g * V + e) * LANES] = sg[g][e];
+                    own[(E + g * V + e) * LANES] = sb[g][e];
+                }
+            own[EPL * LANES] = last_sg;
+            own[(E + EPL) * LANES] = last_sb;
+        }
+        if (ROWS > 1) __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int r = 0; r < ROWS - 1; ++r) {
+            const float* other = lds + r * ENTRIES + mine.lane;
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sg[g][e] += other[(g * V + e) * LANES];
+                    sb[g][e] += other[(E + g * V + e) * LANES];
+                }
+            last_sg += other[EPL * LANES];
+            last_sb += other[(E + EPL) * LANES];
+        }
         float* rows[2] = {to_gamma ? to_gamma + blockIdx.x * stride : nullptr, to_beta ? to_beta + blockIdx.x * stride : nullptr};
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -398,7 +426,7 @@ k_norm_grad_sums(const float* __restrict__ grad_x, const TS* __restrict__ h, con
     }
 }
 
-// grad_h of a tile, and the tile's sums of grad_x n and grad_x over its rows into part[blockIdx.y][2][d].  A lane has 4 columns.  grid (columns, rows)
+// grad_h of a tile, and the tile's sums of grad_x n and grad_x over its rows into part[blockIdx.y][2][d] (with one part: the gradients themselves).  A lane has 4 columns.  grid (columns, rows)
 constexpr int TILE_NT = 256, TILE_COLS = TILE_NT * 4, TILE_AT_ONCE = 8, TILE_ROWS = 2048 /* their statistics take 32 KB of LDS */;
 __device__ __forceinline__ void load_four(const float* p, float (&v)[4]) { load_vec(p, v); }
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -410,12 +438,12 @@ __device__ __forceinline__ void load_four(const uint16_t* p, float (&v)[4]) {
 template <typename TS>
 __global__ void __launch_bounds__(TILE_NT)
 k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, const float* __restrict__ gamma, const float* __restrict__ mean_in,
-                 const float* __restrict__ rstd_in, const float* __restrict__ sums, int splits, float* __restrict__ grad_h, float* __restrict__ part, int b, int d,
-                 int rows) {
+                 const float* __restrict__ rstd_in, const float* __restrict__ sums, int splits, float* __restrict__ grad_h, float* __restrict__ to_gamma, float* __restrict__ to_beta,
+                 size_t stride, int b, int d, int rows) {
     extern __shared__ __align__(16) float of_row[];   // [rows][4]: mean, rstd, mean of u, mean of u n
     const int i0 = (int)blockIdx.y * rows, n = min(rows, b - i0), lane = threadIdx.x & 63;
-    const int c = (int)blockIdx.x * TILE_COLS + (int)threadIdx.x * 4;
-    const bool full = (int)(blockIdx.x + 1) * TILE_COLS <= d;   // the same for the workgroup
+    const int start = (int)blockIdx.x * TILE_COLS + (int)threadIdx.x * 4, c = min(start, max(d - 4, 0));   // (the last lane takes the last four: a neighbour's again)
+    const bool full = d >= 4;
     float gx[2][TILE_AT_ONCE][4], v[2][TILE_AT_ONCE][4], w[4] = {1.f, 1.f, 1.f, 1.f}, sg[4] = {}, sb[4] = {};
     // (loads without conditions, which the compiler would wait for: what is not there is another row's or column's)
     auto load = [&](int r0, float (&g)[TILE_AT_ONCE][4], float (&x)[TILE_AT_ONCE][4]) {
@@ -456,6 +484,7 @@ k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, con
         }
     }
     __syncthreads();
+    if (start >= d) return;
     auto put = [&](float* to, const float (&o)[4]) {
         if (full) store_vec(to + c, o);
         else
@@ -485,9 +514,8 @@ k_norm_grad_tile(const float* __restrict__ grad_x, const TS* __restrict__ h, con
         load(r0 + 2 * TILE_AT_ONCE, gx[0], v[0]);
         work(r0 + TILE_AT_ONCE, gx[1], v[1]);
     }
-    if (!part) return;
-    put(part + ((size_t)blockIdx.y * 2) * d, sg);
-    put(part + ((size_t)blockIdx.y * 2 + 1) * d, sb);
+    if (to_gamma) put(to_gamma + blockIdx.y * stride, sg);
+    if (to_beta) put(to_beta + blockIdx.y * stride, sb);
 }
 
 // The parts' sums, added up in a fixed order: a lane takes COLS columns of one of the two sums and every GROUPS-th part, the groups join through LDS.
@@ -573,11 +601,12 @@ struct NormShape {
 static NormShape norm_shape(const usl_ctx* c, int b) {
     NormShape s = {};
     const int d = c->d, es = c->storage == USL_F32 ? 4 : 2;
-    s.lanes = d <= 128 ? 16 : d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
+    s.lanes = d <= 128 ? 16 : d <= 1024 ? 64 : d <= 2048 ? 128 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
     const int at_once = BWD_NT / s.lanes, all = (b + at_once - 1) / at_once;
     s.parts = all < c->num_cu ? all : c->num_cu;
     // The sums that a workgroup leaves are written and read once: 16 bytes a column and workgroup, against 4 + es bytes a value for reading the inputs again.
-    s.registers = d <= 16384 && d * es >= 16 && (s.parts == 1 || (int64_t)s.parts * 16 <= (int64_t)b * (4 + es));
+    // Below half a million values neither counts, and one pass is a launch less (10 x 4840 bfloat16: 16.4 us and SMALL).
+    s.registers = d <= 16384 && d * es >= 16 && ((int64_t)s.parts * 16 <= (int64_t)b * (4 + es) || (int64_t)b * d <= 1 << 19);
     if (s.registers) return s;
     const int tiles = (d + TILE_COLS - 1) / TILE_COLS, want = (c->num_cu * 2 + tiles - 1) / tiles;
     s.rows = (b + want - 1) / want;
@@ -602,14 +631,14 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
     const size_t held = (size_t)(parts_most < c->max_b ? parts_most : c->max_b) * 2 * d;
     if (!s.registers || (sums && s.parts > 1))
         USL_TRY(usl_reserve(c, (void**)&c->norm_part, &c->norm_part_cap, (held + 2 * ((size_t)c->max_b + 2 * c->num_cu)) * 4));
+    const bool direct = s.parts == 1;
+    float* to_gamma = !sums ? nullptr : direct ? grad_gamma : c->norm_part;
+    float* to_beta = !sums ? nullptr : direct ? grad_beta : c->norm_part + d;
     if (s.registers) {
-        const bool direct = s.parts == 1;
-        float* to_gamma = !sums ? nullptr : direct ? grad_gamma : c->norm_part;
-        float* to_beta = !sums ? nullptr : direct ? grad_beta : c->norm_part + d;
 #define USL_NORM_GRAD(LANES, EPL) do { if (gamma) USL_NORM_GRAD_W(LANES, EPL, true); else USL_NORM_GRAD_W(LANES, EPL, false); } while (0)
 #define USL_NORM_GRAD_W(LANES, EPL, WEIGHT)                                                                                                                      \
     do {                                                                                                                                               \
-        constexpr size_t lds = LANES == BWD_NT ? 0 : (size_t)BWD_NT * 2 * (EPL + 1) * 4;                                                                      \
+        constexpr size_t lds = (size_t)(LANES >= 256 ? BWD_NT - LANES : BWD_NT) * 2 * (EPL + 1) * 4;                                                                      \
         if (lds >= 65536)                                                                                                                              \
             USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(k_norm_grad<TS, LANES, EPL, WEIGHT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
         hipLaunchKernelGGL((k_norm_grad<TS, LANES, EPL, WEIGHT>), dim3((unsigned)s.parts), dim3(BWD_NT), lds, c->stream, grad_x, (const TS*)h, gamma, mean,     \
@@ -618,6 +647,7 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
         if (d <= 128) USL_NORM_GRAD(16, 8);
         else if (d <= 512) USL_NORM_GRAD(64, 8);
         else if (d <= 1024) USL_NORM_GRAD(64, 16);
+        else if (d <= 2048) USL_NORM_GRAD(128, 16);
         else if (d <= 4096) USL_NORM_GRAD(256, 16);
         else if (d <= 8192) USL_NORM_GRAD(512, 16);
         else USL_NORM_GRAD(1024, 16);
@@ -632,9 +662,9 @@ static usl_status norm_grad(usl_ctx* c, const float* grad_x, const void* h, cons
         if (gamma) hipLaunchKernelGGL((k_norm_grad_sums<TS, true>), grid, dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
         else hipLaunchKernelGGL((k_norm_grad_sums<TS, false>), grid, dim3(SUMS_NT), 0, c->stream, grad_x, (const TS*)h, gamma, mean, rstd, row_sums, d, cols);
         hipLaunchKernelGGL(k_norm_grad_tile<TS>, dim3((unsigned)tiles, (unsigned)s.parts), dim3(TILE_NT), (size_t)s.rows * 16, c->stream, grad_x, (const TS*)h, gamma,
-                           mean, rstd, row_sums, s.splits, grad_h, sums ? c->norm_part : nullptr, b, d, s.rows);
+                           mean, rstd, row_sums, s.splits, grad_h, to_gamma, to_beta, (size_t)2 * d, b, d, s.rows);
         USL_TRY(usl_check_launch(c, "layer_norm_backward"));
-        if (!sums) return USL_OK;
+        if (!sums || direct) return USL_OK;
     }
     // few sets of long sums, or many of short ones
     if (s.parts <= 32 && d >= 4)

@@ -24,6 +24,11 @@
 
 namespace usl_products {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 struct Geom {
     int row_bytes;         // bytes from one group's row to the next in the interleaved activations (a multiple of 16)
     int tile_rows;         // rows staged together (small rows)
@@ -436,14 +441,21 @@ struct Mx4Row {
     float scale[(K + 31) / 32];
     __device__ __forceinline__ void load(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t j, bool valid, int k) {
         const int nw = mx4_words(k), nb = mx4_blocks(k);
+        const int64_t row = valid ? j : 0;   // (loads without conditions, which the compiler would wait for one by one)
+        uint32_t byte[(K + 31) / 32];
 #pragma unroll
-        for (int q = 0; q < K / 8; ++q) code[q] = valid && q < nw ? codes[j * nw + q] : 0u;
+        for (int q = 0; q < K / 8; ++q) code[q] = codes[row * nw + min(q, nw - 1)];
 #pragma unroll
-        for (int q = 0; q < (K + 31) / 32; ++q) scale[q] = mx4_scale(valid && q < nb ? scales[j * nb + q] : 127u);
+        for (int q = 0; q < (K + 31) / 32; ++q) byte[q] = scales[row * nb + min(q, nb - 1)];
+#pragma unroll
+        for (int q = 0; q < K / 8; ++q) code[q] = valid && q < nw ? code[q] : 0u;
+#pragma unroll
+        for (int q = 0; q < (K + 31) / 32; ++q) scale[q] = mx4_scale(valid ? byte[q] : 127u);
     }
     __device__ __forceinline__ float at(const uint32_t* mine, int slot, int k) const {
         const float s = K > 32 && slot >= 32 ? scale[K > 32 ? 1 : 0] : scale[0];
-        return slot < k ? mx4_code(mine[slot >> 3] >> (4 * (slot & 7))) * s : 0.f;   // (a padding slot's weight is 0 whatever the scale)
+        const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(mine[slot >> 3] >> (4 * (slot & 7)), 1.f, 0);
+        return slot < k ? v.x * s : 0.f;   // (a padding slot's weight is 0 whatever the scale)
     }
     __device__ __forceinline__ uint32_t* put(uint32_t* lds) const {
         uint32_t* mine = lds + (threadIdx.x >> 6) * 64 * halves_stride<K>() + (threadIdx.x & 63) * (K / 8 + 1);
@@ -527,11 +539,6 @@ __device__ __forceinline__ void store_rows(const float (&acc)[K], float* __restr
 }
 
 // --------------------------------------------------------------------------------------------- gathers
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 template <typename TS, int Q> struct Unit;                      // what one LDS read brings: Q instances of one column
 template <> struct Unit<float, 1> { typedef float T; };
 template <> struct Unit<float, 2> { typedef f32x2 T; };
@@ -786,8 +793,9 @@ template <typename TS, int K> struct WReg;                      // weights of on
 template <int K> struct WReg<float, K> { float v[K]; };
 template <int K> struct WReg<uint16_t, K> { uint32_t v[K / 2]; };
 template <int K> struct WCodes { uint32_t v[K / 8]; float scale; };   // ... as codes of one block
-// Labels of one block keep their codes: 4 bits a slot where float32 takes 32, so a lane has twice the labels, and half the workgroups copy the rows.
-template <int K, bool MX4> constexpr bool keeps_codes() { return MX4 && K <= 32; }
+// Labels of one block may keep their codes, 4 bits a slot where float32 takes 32: a lane then has twice the labels, and half the workgroups copy the rows.
+// Decoding them is half an instruction a gather more, so with fewer labels they are decoded once.
+template <int K, int LPT, bool MX4> constexpr bool keeps_codes() { return MX4 && K <= 32 && LPT > 1 && LPT * K > 64; }
 
 __device__ __forceinline__ uint32_t lds_base(const void* p) {
     return (uint32_t)(uintptr_t)((const __attribute__((address_space(3))) void*)p);
@@ -832,7 +840,7 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
         if (threadIdx.x < (n & 3)) to[(n & ~(size_t)3) + threadIdx.x] = 0.f;
     }
     uint32_t pk[LPT][K / 2];
-    constexpr bool CODES = keeps_codes<K, MX4>();
+    constexpr bool CODES = keeps_codes<K, LPT, MX4>();
     typename std::conditional<CODES, WCodes<K>, WReg<TS, K>>::type w[LPT];
 #pragma unroll
     for (int l = 0; l < LPT; ++l) {
@@ -841,7 +849,7 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
             Mx4Row<K> row;
             row.load(reinterpret_cast<const uint32_t*>(W), scales, row0 + threadIdx.x, row0 + threadIdx.x < end, k);
             SlotOrder<K> so;
-            if constexpr (raw_rows<TS, K, NT>() && !CODES) {
+            if constexpr (raw_rows<TS, K, NT>() && LPT == 1) {
                 RawRows<TS, K> raw;
                 raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
                 unpack_idx<K, TS>(raw, k, reinterpret_cast<uint32_t*>(lds_raw), pk[l]);
@@ -850,12 +858,10 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 so.load(perm, row0 + threadIdx.x, row0 + threadIdx.x < end);
                 fetch_idx<K>(idx, row0, end, k, (uint32_t)tg.zero_col, reinterpret_cast<uint32_t*>(lds_raw), so, pk[l]);
             }
-            if constexpr (CODES) keep_packed(pk[l]);
+            keep_packed(pk[l]);
             row.unpack(reinterpret_cast<uint32_t*>(lds_raw), so, k, w[l].v);
-            if constexpr (CODES) {
-                w[l].scale = row.scale[0];
-                __builtin_amdgcn_sched_barrier(0);   // one label after the other: several at a time would not fit beside those that are resident
-            }
+            if constexpr (CODES) w[l].scale = row.scale[0];
+            __builtin_amdgcn_sched_barrier(0);   // one label after the other: several at a time would not fit beside those that are resident
         } else if constexpr (raw_rows<TS, K, NT>()) {
             RawRows<TS, K> raw;
             raw.load_idx(perm, idx, row0, end, k, (uint32_t)tg.zero_col);
