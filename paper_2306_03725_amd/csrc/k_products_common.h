@@ -475,7 +475,7 @@ struct Mx4Row {
                 const int slot = so.at(8 * q + u);
                 c[q] |= slot < k ? (mine[slot >> 3] >> (4 * (slot & 7)) & 15u) << (4 * u) : 0u;
             }
-            asm volatile("" : "+v"(c[q]));   // here, not where it is first used: eight registers instead of one until then
+            asm volatile("" : "+v"(c[q]));   // made here, not where it is first used: eight registers instead of one until then
         }
         wave_sync();
     }
@@ -484,6 +484,7 @@ struct Mx4Row {
 #pragma unroll
         for (int s = 0; s < K; ++s) {
             w[s] = at(mine, so.at(s), k);
+            asm volatile("" : "+v"(w[s]));   // here, not where it is first used
             if ((s & 7) == 7) __builtin_amdgcn_sched_barrier(0);
         }
         wave_sync();
@@ -493,6 +494,7 @@ struct Mx4Row {
 #pragma unroll
         for (int q = 0; q < K / 2; ++q) {
             wp[q] = __float_as_uint(at(mine, so.at(2 * q), k)) >> 16 | (__float_as_uint(at(mine, so.at(2 * q + 1), k)) & 0xFFFF0000u);
+            asm volatile("" : "+v"(wp[q]));
             if ((q & 3) == 3) __builtin_amdgcn_sched_barrier(0);
         }
         wave_sync();
