@@ -796,8 +796,9 @@ template <int K> struct WReg<float, K> { float v[K]; };
 template <int K> struct WReg<uint16_t, K> { uint32_t v[K / 2]; };
 template <int K> struct WCodes { uint32_t v[K / 8]; float scale; };   // ... as codes of one block
 // Labels of one block may keep their codes, 4 bits a slot where float32 takes 32: a lane then has twice the labels, and half the workgroups copy the rows.
-// Decoding them is half an instruction a gather more, so with fewer labels they are decoded once.
-template <int K, int LPT, bool MX4> constexpr bool keeps_codes() { return MX4 && K <= 32 && LPT > 1 && LPT * K > 64; }
+// Decoding them is half an instruction a gather more, so with fewer labels they are decoded once.  Not labels of up to 16 slots, which share the registers
+// with their scores (m = 602k, d = 2.9k, k = 8, b = 260, bfloat16: 187 us with eight labels a lane, 156 with four).
+template <int K, int LPT, bool MX4> constexpr bool keeps_codes() { return MX4 && K > 16 && K <= 32 && LPT * K > 64; }
 
 __device__ __forceinline__ uint32_t lds_base(const void* p) {
     return (uint32_t)(uintptr_t)((const __attribute__((address_space(3))) void*)p);

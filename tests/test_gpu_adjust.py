@@ -274,3 +274,36 @@ def test_another_stream_and_a_graph(usl):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((lab, val, got), want)), turn
+
+
+# short segments by themselves and runs of long ones, few and many candidates to merge, batches that fill the chip more than once
+PATHS = [(6552, 189, 10), (20000, 300, 5), (46472, 92, 1), (58262, 49, 32), (100000, 100, 32), (100001, 1100, 3), (500000, 1, 32), (747351, 57, 5), (1761053, 2, 32), (2900000, 1, 32),
+         (4300003, 1, 32), (4096, 1500, 32)]
+
+
+@pytest.mark.parametrize("order", ["any", "rising", "falling", "equal"])
+@pytest.mark.parametrize("m,b,kk", PATHS)
+def test_scores_in_any_order(usl, m, b, kk, order):
+    """Scores in any order, rising with the label (every segment is better than those before), falling, all equal; against a stable sort."""
+    print("order", m, b, kk, order, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(m + kk)
+    if order == "any":
+        out = torch.randn((b, m), device="cuda", generator=gen)
+    elif order == "equal":
+        out = torch.full((b, m), 0.5, device="cuda")
+    else:
+        out = torch.arange(m, device="cuda", dtype=torch.float32).mul_(1.0 if order == "rising" else -1.0).repeat(b, 1)
+    words = torch.randint(-2 ** 31, 2 ** 31, ((m + 31) // 32,), device="cuda", generator=gen, dtype=torch.int64).to(torch.int32)
+    allowed = ((words[:, None] >> torch.arange(32, device="cuda", dtype=torch.int32)) & 1).view(-1)[:m] != 0
+    L = usl.Layer(m, 1, 1, b)
+    lab, val = torch.empty((b, kk), dtype=torch.int32, device="cuda"), torch.empty((b, kk), device="cuda")
+    for mask in (None, words[None, :]):
+        L.topk_adjusted(out, usl.Adjustments(allowed=mask), b, kk, lab, val)
+        for i in {0, b // 2, b - 1}:
+            z = out[i] if mask is None else torch.where(allowed, out[i], -float("inf"))
+            want, at = z.sort(descending=True, stable=True)
+            assert torch.equal(lab[i].long(), at[:kk]) and torch.equal(val[i], want[:kk]), (i, mask is None)
+    if order != "equal":
+        L.topk(out, b, kk, lab, val)
+        want, at = out[b - 1].sort(descending=True, stable=True)
+        assert torch.equal(lab[b - 1].long(), at[:kk]) and torch.equal(val[b - 1], want[:kk])
