@@ -4,6 +4,8 @@
 // the row in LDS, and the LPL lanes of a label add up their sums; after LPL rounds every lane has a label's.  A round of the whole grid is a run of
 // consecutive labels, 64 / LPL to a wavefront.  A round's first label is the same for the wavefront, so addresses are scalar bases and 32-bit offsets that never
 // change; what would lie behind the last label begins earlier (labels that two wavefronts share get the same bits twice).
+// Bound by the stream of idx and codes: m = 670k, k = 64, b = 1, bfloat16: 197 MB in 39.6 us, 5.0 TB/s, the rate of a large copy (31 us where they are still in the
+// cache behind the L2s; with runs of 64 labels to a wavefront 41, and 33).
 // Labels of up to 32 slots are one block: their sums are scaled once, where a lane has its label's.
 #pragma once
 #include "k_products_common.h"

@@ -106,7 +106,8 @@ __device__ __forceinline__ T block_sum(T v, T* red) {
 }
 
 // ---- forward: a row in the registers of LANES lanes, EPL values each (and one of the values behind the groups) --
-// Read once, written once.  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
+// Read once, written once; bound by that stream where there are many rows (512 x 32768 bfloat16: 67 MB in 14.9 us, 4.5 TB/s where a large copy
+// reaches 5.0), by one launch's latency where there are few (1 x 32768 float32: 6.0 us).  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
 // around the row's mean, behind one barrier:  M2 = sum_w M2_w + n_w (mean_w - mean)^2.
 // FULL: there are both a weight and a bias; EARLY: they come with the row, not behind the sums.
 template <typename TS, int LANES, int EPL, bool FULL, bool EARLY>
@@ -230,7 +231,9 @@ k_norm_any(const TS* h, const float* __restrict__ gamma, const float* __restrict
 
 // ---- backward, rows of up to 16384: a row in the registers of LANES lanes, EPL values each -----------------------
 // A workgroup of 1024 lanes takes 1024 / LANES rows at a time, its share of the batch one after the other, and keeps the sums of grad_x n and grad_x
-// of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined through LDS, always in the same order, and left in part[workgroup][2][d] (with one workgroup: in the gradients themselves).
+// of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined through LDS, always in the same order, and left in
+// part[workgroup][2][d] (with one workgroup: in the gradients themselves).  Bound by the wait for the rows, which every wavefront has once or a few
+// times, and by the launch that adds the parts up: 4099 x 1003 bfloat16, 41 MB: 11.4 + 3.5 us, 8.3 at the rate of a large copy.
 // WEIGHT: there is a gamma.
 constexpr int BWD_NT = 1024;
 template <typename TS, int LANES, int EPL, bool WEIGHT>
@@ -374,7 +377,9 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
 }
 
 // ---- backward, wide rows: the rows' sums first, then tiles of columns and rows -----------------------------------
-// The inputs are read twice, the second time mostly from the cache behind the L2s.
+// The inputs are read twice, the second time mostly from the cache behind the L2s, and that is what bounds it: 256 x 32768 float32: sums 12.5 us (67 MB),
+// tiles 17.4 (101 MB), parts 3.9; one pass would be 20.3 at the rate of a large copy.  (A row of this width and its sums of columns do not fit the registers
+// of a compute unit beside each other, and sums left by every row are as many bytes as the inputs.)
 // sums[i][split][2]: sums of u and u n over a share of row i's columns.  grid (splits, rows)
 constexpr int SUMS_NT = 512;
 template <typename TS, bool WEIGHT>
@@ -556,40 +561,53 @@ k_norm_sum_parts(const float* __restrict__ part, int parts, int d, float* __rest
 
 }  // namespace
 
+struct NormArgs {
+    const void* h;
+    const float *gamma, *beta;
+    float eps;
+    void* x;
+    float *mean, *rstd;
+    int32_t b;
+};
+template <typename TS, int LANES, int EPL, bool FULL, bool EARLY>
+static void launch_norm(usl_ctx* c, const NormArgs& a) {
+    constexpr int NT = LANES < 256 ? 256 : LANES, ROWS = NT / LANES;
+    hipLaunchKernelGGL((k_norm<TS, LANES, EPL, FULL, EARLY>), dim3((unsigned)((a.b + ROWS - 1) / ROWS)), dim3(NT), 0, c->stream, (const TS*)a.h, a.gamma, a.beta, a.eps,
+                       (TS*)a.x, a.mean, a.rstd, a.b, c->d);
+}
+// Weight and bias come with the row where registers are left for them: always for 16 values a lane, never for 64; for 32 where there is at most one row to a compute
+// unit, whose wait for them nothing else covers (1 x 32768 float32 6.5 us, early 6.0; 512 x 32768 bfloat16, two rows to a compute unit: 14.9, early, one, 17.7).
+template <typename TS, int LANES, int EPL>
+static void launch_norm(usl_ctx* c, const NormArgs& a) {
+    if (!a.gamma || !a.beta) return launch_norm<TS, LANES, EPL, false, false>(c, a);
+    if constexpr (EPL <= 16) launch_norm<TS, LANES, EPL, true, true>(c, a);
+    else if constexpr (EPL > 32) launch_norm<TS, LANES, EPL, true, false>(c, a);
+    else if (a.b <= c->num_cu) launch_norm<TS, LANES, EPL, true, true>(c, a);
+    else launch_norm<TS, LANES, EPL, true, false>(c, a);
+}
 // Lanes of a row by its length: 16 where four rows fit a wavefront, then a wavefront, then as many as keep 16 values each; the longest rows of a
 // workgroup have 32 or 64 values a lane.
 template <typename TS>
-static usl_status norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b) {
-#define USL_NORM(LANES, EPL)                                                                         \
-    do {                                                                                             \
-        if (!gamma || !beta) USL_NORM_F(LANES, EPL, false, false);                                   \
-        else if (EPL <= 16 || (EPL == 32 && b <= c->num_cu)) USL_NORM_F(LANES, EPL, true, (EPL <= 32)); \
-        else USL_NORM_F(LANES, EPL, true, false);                                                    \
-    } while (0)
-#define USL_NORM_F(LANES, EPL, FULL, EARLY)                                                                                         \
-    hipLaunchKernelGGL((k_norm<TS, LANES, EPL, FULL, EARLY>), dim3((unsigned)((b + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1))), \
-                       dim3(LANES < 256 ? 256 : LANES), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, b, c->d)
-#define USL_NORM_ANY hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)b), dim3(ANY_NT), 0, c->stream, (const TS*)h, gamma, beta, eps, (TS*)x, mean, rstd, c->d)
-    if (c->d < VEC<TS>) USL_NORM_ANY;
-    else if (c->d <= 128) USL_NORM(16, 8);
-    else if (c->d <= 256) USL_NORM(16, 16);
-    else if (c->d <= 512) USL_NORM(64, 8);
-    else if (c->d <= 1024) USL_NORM(64, 16);
-    else if (c->d <= 2048) USL_NORM(64, 32);
-    else if (c->d <= 4096) USL_NORM(256, 16);
-    else if (c->d <= 8192) USL_NORM(512, 16);
-    else if (c->d <= 16384) USL_NORM(1024, 16);
-    else if (c->d <= 32768) USL_NORM(1024, 32);
-    else if (c->d <= 65536) USL_NORM(1024, 64);
-    else USL_NORM_ANY;
-#undef USL_NORM_ANY
-#undef USL_NORM_F
-#undef USL_NORM
+static usl_status norm(usl_ctx* c, const NormArgs& a) {
+    const int d = c->d;
+    if (d < VEC<TS> || d > 65536)
+        hipLaunchKernelGGL(k_norm_any<TS>, dim3((unsigned)a.b), dim3(ANY_NT), 0, c->stream, (const TS*)a.h, a.gamma, a.beta, a.eps, (TS*)a.x, a.mean, a.rstd, d);
+    else if (d <= 128) launch_norm<TS, 16, 8>(c, a);
+    else if (d <= 256) launch_norm<TS, 16, 16>(c, a);
+    else if (d <= 512) launch_norm<TS, 64, 8>(c, a);
+    else if (d <= 1024) launch_norm<TS, 64, 16>(c, a);
+    else if (d <= 2048) launch_norm<TS, 64, 32>(c, a);
+    else if (d <= 4096) launch_norm<TS, 256, 16>(c, a);
+    else if (d <= 8192) launch_norm<TS, 512, 16>(c, a);
+    else if (d <= 16384) launch_norm<TS, 1024, 16>(c, a);
+    else if (d <= 32768) launch_norm<TS, 1024, 32>(c, a);
+    else launch_norm<TS, 1024, 64>(c, a);
     return usl_check_launch(c, "layer_norm");
 }
 
 usl_status usl_launch_norm(usl_ctx* c, const void* h, const float* gamma, const float* beta, float eps, void* x, float* mean, float* rstd, int32_t b) {
-    return c->storage == USL_F32 ? norm<float>(c, h, gamma, beta, eps, x, mean, rstd, b) : norm<uint16_t>(c, h, gamma, beta, eps, x, mean, rstd, b);
+    const NormArgs a = {h, gamma, beta, eps, x, mean, rstd, b};
+    return c->storage == USL_F32 ? norm<float>(c, a) : norm<uint16_t>(c, a);
 }
 
 // How the backward pass is cut up.
@@ -605,7 +623,7 @@ static NormShape norm_shape(const usl_ctx* c, int b) {
     const int at_once = BWD_NT / s.lanes, all = (b + at_once - 1) / at_once;
     s.parts = all < c->num_cu ? all : c->num_cu;
     // The sums that a workgroup leaves are written and read once: 16 bytes a column and workgroup, against 4 + es bytes a value for reading the inputs again.
-    // Below half a million values neither counts, and one pass is a launch less (10 x 4840 bfloat16: 16.4 us and SMALL).
+    // Below half a million values neither counts, and one pass is a launch less (10 x 4840 bfloat16: 16.4 us and 10.8).
     s.registers = d <= 16384 && d * es >= 16 && ((int64_t)s.parts * 16 <= (int64_t)b * (4 + es) || (int64_t)b * d <= 1 << 19);
     if (s.registers) return s;
     const int tiles = (d + TILE_COLS - 1) / TILE_COLS, want = (c->num_cu * 2 + tiles - 1) / tiles;
