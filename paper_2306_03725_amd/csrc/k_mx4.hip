@@ -164,7 +164,7 @@ k_mx4_forward_any(const TS* __restrict__ x, const int32_t* __restrict__ idx, con
 
 }  // namespace
 
-// m = 500k, k = 32, float32, both calls one after the other: 137 MB in 29.9 us, 4.6 TB/s, where a large copy reaches 5.0.  (A lane a block of 32, its slots
+// m = 500k, k = 32, float32, both calls one after the other: 137 MB in 30.2 us, 4.5 TB/s, where a large copy reaches 5.0.  (A lane a block of 32, its slots
 // one after the other, took 544.)
 usl_status usl_launch_mx4_quantize(usl_ctx* c, const void* W, uint32_t* codes, uint8_t* scales) {
     const int per = lanes_of_label(c->k);

@@ -106,8 +106,8 @@ __device__ __forceinline__ T block_sum(T v, T* red) {
 }
 
 // ---- forward: a row in the registers of LANES lanes, EPL values each (and one of the values behind the groups) --
-// Read once, written once; bound by that stream where there are many rows (512 x 32768 bfloat16: 67 MB in 14.9 us, 4.5 TB/s where a large copy
-// reaches 5.0), by one launch's latency where there are few (1 x 32768 float32: 6.0 us).  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
+// Read once, written once; bound by that stream where there are many rows (512 x 32768 bfloat16: 67 MB in 15.1 us, 4.5 TB/s where a large copy
+// reaches 5.0), by one launch's latency where there are few (1 x 32768 float32: 5.9 us).  A wavefront takes the mean and the squared deviations of its own values; several wavefronts of a row join theirs
 // around the row's mean, behind one barrier:  M2 = sum_w M2_w + n_w (mean_w - mean)^2.
 // FULL: there are both a weight and a bias; EARLY: they come with the row, not behind the sums.
 template <typename TS, int LANES, int EPL, bool FULL, bool EARLY>
@@ -233,7 +233,7 @@ k_norm_any(const TS* h, const float* __restrict__ gamma, const float* __restrict
 // A workgroup of 1024 lanes takes 1024 / LANES rows at a time, its share of the batch one after the other, and keeps the sums of grad_x n and grad_x
 // of its rows in registers: the inputs are read once.  At the end its row groups' sums are joined through LDS, always in the same order, and left in
 // part[workgroup][2][d] (with one workgroup: in the gradients themselves).  Bound by the wait for the rows, which every wavefront has once or a few
-// times, and by the launch that adds the parts up: 4099 x 1003 bfloat16, 41 MB: 11.4 + 3.5 us, 8.3 at the rate of a large copy.
+// times, and by the launch that adds the parts up: 4099 x 1003 bfloat16, 41 MB: 14.7 us (kernels 12.0 + 3.8 in a trace), 8.3 at the rate of a large copy.
 // WEIGHT: there is a gamma.
 constexpr int BWD_NT = 1024;
 template <typename TS, int LANES, int EPL, bool WEIGHT>
@@ -377,8 +377,8 @@ k_norm_grad(const float* __restrict__ grad_x, const TS* __restrict__ h, const fl
 }
 
 // ---- backward, wide rows: the rows' sums first, then tiles of columns and rows -----------------------------------
-// The inputs are read twice, the second time mostly from the cache behind the L2s, and that is what bounds it: 256 x 32768 float32: sums 12.5 us (67 MB),
-// tiles 17.4 (101 MB), parts 3.9; one pass would be 20.3 at the rate of a large copy.  (A row of this width and its sums of columns do not fit the registers
+// The inputs are read twice, the second time mostly from the cache behind the L2s, and that is what bounds it: 256 x 32768 float32: 34.0 us (in a trace sums
+// 13.5, 67 MB, tiles 18.4, 101 MB, parts 4.3); one pass would be 20.3 at the rate of a large copy.  (A row of this width and its sums of columns do not fit the registers
 // of a compute unit beside each other, and sums left by every row are as many bytes as the inputs.)
 // sums[i][split][2]: sums of u and u n over a share of row i's columns.  grid (splits, rows)
 constexpr int SUMS_NT = 512;
