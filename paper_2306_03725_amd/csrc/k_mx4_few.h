@@ -6,7 +6,9 @@
 // change; what would lie behind the last label begins earlier (labels that two wavefronts share get the same bits twice).
 // Bound by the stream of idx and codes: m = 670k, k = 64, b = 1, bfloat16: 197 MB in 39.6 us, 5.0 TB/s, the rate of a large copy (31 us where they are still in the
 // cache behind the L2s; with runs of 64 labels to a wavefront 41, and 33).
-// Labels of up to 32 slots are one block: their sums are scaled once, where a lane has its label's.
+// The scale is the conversion's operand, so that every weight is what usl_dequantize_mx4 makes of it and the sums have usl_forward's range (sums of codes, scaled at the
+// end, do not).  It comes with its piece; where that is six loads already (APART), a label's scale is loaded a turn ahead by the lane that ends with its sum, and
+// handed to the others by a permutation (m = 500k, d = 32k, k = 30, b = 1, bfloat16: 19.4 us, with a load a piece 21.1; k = 32, with it, 13.6).
 #pragma once
 #include "k_products_common.h"
 
@@ -21,7 +23,7 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
           float* __restrict__ out, int64_t m, int k_, int b, int row_bytes) {
     typedef typename Unit<TS, Q>::T U;
     constexpr int R = 64 / LPL;              // labels of a round
-    constexpr bool ONE_BLOCK = LPL <= 8;
+    constexpr bool APART = SLOTS == MX4_ANY_SLOTS && LPL <= 8;
     extern __shared__ __align__(16) unsigned char lds_raw[];
     const uint32_t lds0 = lds_base(lds_raw);
     const int k = SLOTS == MX4_ALL_SLOTS ? 4 * LPL : k_, words = mx4_words(k), blocks = mx4_blocks(k);
@@ -50,9 +52,9 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
             p.c[0] = c.x; p.c[1] = c.y; p.c[2] = c.z; p.c[3] = c.w;
         }
         p.w = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(codes + j * words) + word_at);
-        if (!ONE_BLOCK) p.s = (scales + j * blocks)[scale_at];
+        if (!APART) p.s = (scales + j * blocks)[scale_at];
     };
-    auto dot4 = [&](const Piece& p, float (&acc)[Q]) {
+    auto dot4 = [&](const Piece& p, float scale, float (&acc)[Q]) {
         U v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = lds_read<U>(lds0 + (SLOTS != MX4_ALL_SLOTS && t + q >= k ? nowhere : p.c[q]) * (uint32_t)sizeof(U));
@@ -60,7 +62,7 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
 #pragma unroll
         for (int q = 0; q < 4; q += 2) {
             if constexpr (sizeof(TS) == 4) {
-                const f32x2 w = q ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 1) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, 1.f, 0);
+                const f32x2 w = q ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, scale, 1) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(half, scale, 0);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     if constexpr (Q == 1) acc[0] = fmaf(w[u], v[q + u], acc[0]);
@@ -70,8 +72,8 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
                     }
                 }
             } else {
-                const uint32_t w = __builtin_bit_cast(uint32_t, q ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 1)
-                                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, 1.f, 0));
+                const uint32_t w = __builtin_bit_cast(uint32_t, q ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, scale, 1)
+                                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(half, scale, 0));
                 if constexpr (Q == 1) acc[0] = dot2((uint32_t)v[q] | ((uint32_t)v[q + 1] << 16), w, acc[0]);
                 else if constexpr (Q == 2) {
                     acc[0] = dot2(join_lo(v[q], v[q + 1]), w, acc[0]);
@@ -84,31 +86,28 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
                 }
             }
         }
-        if (!ONE_BLOCK) {
-            const float scale = mx4_scale(p.s);
-#pragma unroll
-            for (int i = 0; i < Q; ++i) acc[i] *= scale;
-        }
     };
     const int64_t waves = (int64_t)gridDim.x * nw, wave = (int64_t)blockIdx.x * nw + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int rounds = (int)((m + waves * R - 1) / (waves * R));
     auto first_of = [&](int round) { return min((round * waves + wave) * R, m - R); };
+    auto mine_of = [&](int r0) { return min(((r0 + sub) * waves + wave) * R, m - R) + lane / LPL; };   // the label whose sum this lane ends with, of rounds r0 ... r0 + LPL - 1
+    uint32_t next = 127u;
+    if (APART) next = scales[mine_of(0)];
     Piece p[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) fetch(first_of(a), p[a]);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     for (int r0 = 0; r0 < rounds; r0 += LPL) {
-        const int64_t mine = min(((r0 + sub) * waves + wave) * R, m - R) + lane / LPL;   // the label whose sum this lane ends with
-        uint32_t scale = 127u;
-        if (ONE_BLOCK) scale = scales[mine];
+        const float held = mx4_scale(next);
+        if (APART) next = scales[mine_of(r0 + LPL)];
         float sum[Q] = {};
 #pragma unroll 1
         for (int r1 = 0; r1 < LPL && r0 + r1 < rounds; r1 += AHEAD) {
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
                 float acc[Q] = {};
-                dot4(p[a], acc);
+                dot4(p[a], APART ? __int_as_float(__builtin_amdgcn_ds_bpermute(((lane & ~(LPL - 1)) + r1 + a) * 4, __float_as_int(held))) : mx4_scale(p[a].s), acc);
                 fetch(first_of(r0 + r1 + a + AHEAD), p[a]);   // (behind the last round: the last labels again, and nothing is made of them)
 #pragma unroll
                 for (int i = 0; i < Q; ++i) {   // (lanes that have been added up are alike: a mirror reaches the others as well)
@@ -122,10 +121,10 @@ k_mx4_few(const char* __restrict__ xi, const int32_t* __restrict__ idx, const ui
             }
         }
         if (r0 + sub < rounds) {
-            const float s = ONE_BLOCK ? mx4_scale(scale) : 1.f;
+            const int64_t mine = mine_of(r0);
 #pragma unroll
             for (int i = 0; i < Q; ++i)
-                if (i < b) out[(size_t)i * m + mine] = ONE_BLOCK ? sum[i] * s : sum[i];
+                if (i < b) out[(size_t)i * m + mine] = sum[i];
         }
     }
 }

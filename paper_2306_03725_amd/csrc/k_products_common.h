@@ -464,7 +464,7 @@ struct Mx4Row {
         wave_sync();
         return mine;
     }
-    // ... or as codes, eight to a register, which a label of one block leaves in place (their scale is the sum's)
+    // ... or as codes, eight to a register, which a label of one block leaves in place (and its scale beside them)
     __device__ __forceinline__ void unpack(uint32_t* lds, const SlotOrder<K>& so, int k, uint32_t (&c)[K / 8]) const {
         const uint32_t* mine = put(lds);
 #pragma unroll
@@ -649,9 +649,10 @@ __device__ __forceinline__ void label_dot(const uint32_t (&pk)[K / 2], const uin
     }
 }
 
-// Codes of values in 4 bits, eight to a register: one instruction makes the weights of two steps of them.
+// Codes of values in 4 bits, eight to a register: one instruction makes the weights of two steps of them, scaled.  (The scale is its operand: codes' sums that are
+// scaled at the end leave float32's range where the scores do not.)
 template <int K, typename TS, int Q, bool HALVES>
-__device__ __forceinline__ void label_dot_mx4(const uint32_t (&pk)[K / 2], const uint32_t (&c)[K / 8], uint32_t base, uint32_t zbyte, float (&acc)[Q]) {
+__device__ __forceinline__ void label_dot_mx4(const uint32_t (&pk)[K / 2], const uint32_t (&c)[K / 8], float scale, uint32_t base, uint32_t zbyte, float (&acc)[Q]) {
     constexpr int B = sizeof(TS) == 4 ? batch_of<float, Q>() : 8;
     typedef typename Unit<TS, Q>::T U;
 #pragma unroll
@@ -664,8 +665,8 @@ __device__ __forceinline__ void label_dot_mx4(const uint32_t (&pk)[K / 2], const
             const uint32_t word = c[(t0 + u) / 8];
             const int byte = (t0 + u) % 8 / 2;
             if constexpr (sizeof(TS) == 4) {
-                const f32x2 w = byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 1)
-                              : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 3);
+                const f32x2 w = byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1)
+                              : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     if constexpr (Q == 1) acc[0] = fmaf(w[s], v[u + s], acc[0]);
@@ -675,8 +676,8 @@ __device__ __forceinline__ void label_dot_mx4(const uint32_t (&pk)[K / 2], const
                     }
                 }
             } else {
-                const uint32_t w2 = __builtin_bit_cast(uint32_t, byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 1)
-                                                               : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 2) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, 1.f, 3));
+                const uint32_t w2 = __builtin_bit_cast(uint32_t, byte == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0) : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1)
+                                                               : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
                 if constexpr (Q == 1) acc[0] = dot2((uint32_t)v[u] | ((uint32_t)v[u + 1] << 16), w2, acc[0]);
                 else if constexpr (Q == 2) {
                     acc[0] = dot2(join_lo(v[u], v[u + 1]), w2, acc[0]);
@@ -948,7 +949,6 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 for (int q = 0; q < Q; ++q)
                     if (g * Q + q < b) {
                         float o = z[q];
-                        if constexpr (CODES) o *= w[l].scale;
                         if (LOSS) {
                             const usl_loss_parts r = usl_loss_in_parts(LOSS == 2 ? 1 : loss.kind, o, any_target.value && (hits >> q & 1u) ? 1.f : 0.f, loss.scale);
                             o = r.g;
@@ -992,7 +992,7 @@ k_forward(const char* __restrict__ xi, const int32_t* __restrict__ idx, const TS
                 __builtin_amdgcn_s_setprio(1);
                 if constexpr (CODES) keep_packed(w[l].v);
                 if (!EVEN || wave0 + l * NT < nlab) {
-                    if constexpr (CODES) label_dot_mx4<K, TS, Q, HALVES>(pk[l], w[l].v, base, zbyte, acc);
+                    if constexpr (CODES) label_dot_mx4<K, TS, Q, HALVES>(pk[l], w[l].v, w[l].scale, base, zbyte, acc);
                     else label_dot<K, Q, HALVES>(pk[l], w[l].v, base, zbyte, acc);
                 }
                 __builtin_amdgcn_s_setprio(0);
