@@ -489,7 +489,7 @@ usl_status run_backward_weight_generic(usl_ctx* c, const float* g, const void* x
 
 // ---- the register-resident kernels ---------------------------------------------------------------------------
 
-// tuning and test aids: workgroup shape (0 .. 3) and parts of the batch instead of the estimate's choice; parts of the batch (up to
+// tuning and test aids: workgroup shape (0 .. 5) and parts of the batch instead of the estimate's choice; parts of the batch (up to
 // as many as it has groups) for the last half of forward's blocks of labels, whatever the rounds
 int tune_shape() { const char* e = getenv("USL_TUNE_SHAPE"); return e && *e ? atoi(e) : -1; }
 int tune_split() { const char* e = getenv("USL_TUNE_SPLIT"); return e && *e ? atoi(e) : 0; }

@@ -22,10 +22,11 @@ template <int K, typename TS, int Q, bool HALVES>
 ProductKernel pick(ProductKind kind, int shape) {
     constexpr int L = K == 8 ? 4 : labels_per_lane(K, 64), L2 = labels_per_lane(K, 128);
     constexpr bool WIDE_PAIRS = K == 64 && sizeof(TS) == 2 && Q <= 2;
-    if constexpr (keeps_codes<K, L2, true>()) {   // shapes 4 and 5: twice the labels, whose values are 4 bits each
+    if constexpr (keeps_codes<K, L2, true>()) {   // shapes 4 and 5: twice the labels, whose values are 4 bits each.  (Not 512 lanes with four labels of 32 slots: the estimate never
+                                                  // takes them, with shape 2's labels to a block and half its wavefronts.)
 #define USL_CODES(LPT, NT, EVEN) (const void*)k_forward<K, LPT, NT, TS, Q, HALVES, 0, EVEN, (K <= 16), true>
         if (kind == FORWARD_MX4 && shape == 4) return ProductKernel{USL_CODES(L2, 1024, false), USL_CODES(L2, 1024, true), K, L2, 1024, transpose_bytes<K, 1024>()};
-        if constexpr (Q > 1) {
+        if constexpr (Q > 1 && K < 32) {
             if (kind == FORWARD_MX4 && shape == 5) return ProductKernel{USL_CODES(L2, 512, false), USL_CODES(L2, 512, true), K, L2, 512, transpose_bytes<K, 512>()};
         }
 #undef USL_CODES

@@ -42,3 +42,11 @@ def test_forms_that_keep_codes_by_the_rule(stand_in, m, d, k, b, storage, form):
     run(stand_in, FORM + """
 assert form(%d, %d, %d, %d, "%s") == %r
 """ % (m, d, k, b, storage, form))
+
+
+def test_no_form_that_no_size_reaches(stand_in):   # noqa: F811
+    """512 lanes with four labels of 32 slots each were there and never taken: shape 2 has as many labels to a block and twice the wavefronts."""
+    run(stand_in, FORM + """
+for d, b, storage, q, halves in %r:
+    assert form(6001, d, 32, b, storage, SHAPE=5)[1:3] != (4, 512), (d, b, storage)
+""" % LAYOUTS)
