@@ -15,13 +15,20 @@ constexpr int TK_EPT = 64, TK_EPT_FEW = 8;
 static_assert(TK_NT * TK_EPT_FEW == TOPK_SHORT_SEGMENT, "what the choice of a prediction's path counts with");
 
 // The kk best keys of one segment of 256 * TK_EPT labels of one row, best first, into cand[row][segment][kk]
-// (0 where the segment has fewer than kk labels): every lane loads its TK_EPT scores, all loads in flight at once (best_of_segment).
+// (0 where the segment has fewer than kk labels).
+//   1. every lane loads its TK_EPT scores (all loads in flight at once) and finds its own best key;
+//   2. tau = the kk-th best of the 256 lane maxima: at least kk keys of the segment are >= tau, and
+//      every key >= tau belongs to one of the kk lanes whose maximum is >= tau, so at most kk*TK_EPT keys pass;
+//   3. those keys are collected in LDS and the best kk are peeled off one by one ("largest key below the
+//      previous winner": keys are distinct, so nothing has to be removed).
 // VEC: rows are 16-byte aligned and m % 4 == 0, so a lane reads groups of 4 consecutive labels.
 template <bool VEC, int TK_EPT>
 __global__ void __launch_bounds__(TK_NT)
 k_topk_segments(const float* __restrict__ out, int64_t m, int kk, int nseg, uint64_t* __restrict__ cand) {
-    __shared__ TopkSegment<TK_NT> shared;
+    __shared__ uint64_t red[2][TK_NT / 64];
+    BlockMax<TK_NT> block_max = {red, 0};
     __shared__ uint64_t list[TOPK_MAX * TK_EPT];
+    __shared__ uint32_t count;
     constexpr int TK_SEG = TK_NT * TK_EPT;   // labels per workgroup
     const int64_t seg0 = (int64_t)blockIdx.x * TK_SEG;
     const float* row = out + (int64_t)blockIdx.y * m + seg0;
@@ -46,8 +53,48 @@ k_topk_segments(const float* __restrict__ out, int64_t m, int kk, int nseg, uint
             v[e] = j < lim ? row[j] : 0.f;
         }
     }
-    best_of_segment<TK_NT, TK_EPT>(v, local_of, [&](int, int j) -> bool { return j < lim; }, seg0, kk, shared, list,
-                                   cand + ((size_t)blockIdx.y * nseg + blockIdx.x) * kk);
+    // the lane's best score; labels grow with e, so the first of equal scores is the smaller label
+    float top = 0.f;
+    int top_j = -1;
+#pragma unroll
+    for (int e = 0; e < TK_EPT; ++e) {
+        const int j = local_of(e);
+        const bool better = j < lim && (top_j < 0 || v[e] > top);
+        top = better ? v[e] : top;
+        top_j = better ? j : top_j;
+    }
+    const uint64_t mine = top_j >= 0 ? score_key(top, (uint32_t)(seg0 + top_j)) : 0ull;
+    uint64_t tau = ~0ull;
+    for (int r = 0; r < kk && tau != 0; ++r) tau = block_max(mine < tau ? mine : 0ull);
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    // keys are built only for scores that reach tau's score (a cheap float test first)
+    const uint32_t tu = (uint32_t)(tau >> 32);
+    const float tau_score = tau == 0 ? -INFINITY : __uint_as_float((tu & 0x80000000u) ? (tu & 0x7FFFFFFFu) : ~tu);
+#pragma unroll
+    for (int e = 0; e < TK_EPT; ++e) {
+        const int j = local_of(e);
+        if (j < lim && v[e] >= tau_score) {
+            const uint64_t key = score_key(v[e], (uint32_t)(seg0 + j));
+            if (key >= tau) {
+                const uint32_t at = atomicAdd(&count, 1u);
+                if (at < TOPK_MAX * TK_EPT) list[at] = key;   // (more only where a score is NaN, which no key ranks)
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t n = min(count, (uint32_t)(TOPK_MAX * TK_EPT));
+    uint64_t* dst = cand + ((size_t)blockIdx.y * nseg + blockIdx.x) * kk;
+    uint64_t prev = ~0ull;
+    for (int r = 0; r < kk; ++r) {
+        uint64_t best = 0;
+        for (uint32_t q = threadIdx.x; q < n; q += TK_NT) {
+            const uint64_t key = list[q];
+            if (key < prev && key > best) best = key;
+        }
+        prev = block_max(best);
+        if (threadIdx.x == 0) dst[r] = prev;
+    }
 }
 
 // One workgroup per row: the best kk of the row's nseg*kk candidate keys, unpacked.  A launch of its own: merged by the workgroup

@@ -96,63 +96,3 @@ __device__ __forceinline__ uint64_t best_keys(const uint64_t (&held)[HELD], int 
     for (int q = 0; q < (WAVES * TOPK_MAX + 63) / 64; ++q) mine[q] = q * 64 + lane < WAVES * kk ? list[q * 64 + lane] : 0ull;
     return best_keys<1>(mine, kk, list);
 }
-
-template <int NT>
-struct TopkSegment {
-    uint64_t red[2][NT / 64];
-    uint32_t count;
-};
-
-// The kk best keys of the EPT scores that each of a workgroup's lanes holds, best first, into dst[kk] (0 where there are no more).  Register e holds
-// label seg0 + local_of(e), which grows with e, and counts where is(e, local_of(e)); list: TOPK_MAX * EPT places.
-//   1. every lane finds its own best key;
-//   2. tau = the kk-th best of the lanes' maxima: at least kk keys of the segment are >= tau, and
-//      every key >= tau belongs to one of the kk lanes whose maximum is >= tau, so at most kk*EPT keys pass;
-//   3. those keys are collected in LDS and the best kk are peeled off one by one ("largest key below the
-//      previous winner": keys are distinct, so nothing has to be removed).
-template <int NT, int EPT, typename LABEL, typename IS>
-__device__ __forceinline__ void best_of_segment(const float (&v)[EPT], LABEL local_of, IS is, int64_t seg0, int kk, TopkSegment<NT>& shared,
-                                                uint64_t* list, uint64_t* dst) {
-    BlockMax<NT> block_max = {shared.red, 0};
-    // the lane's best score; labels grow with e, so the first of equal scores is the smaller label
-    float top = 0.f;
-    int top_j = -1;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-        const int j = local_of(e);
-        const bool better = is(e, j) && (top_j < 0 || v[e] > top);
-        top = better ? v[e] : top;
-        top_j = better ? j : top_j;
-    }
-    const uint64_t mine = top_j >= 0 ? score_key(top, (uint32_t)(seg0 + top_j)) : 0ull;
-    uint64_t tau = ~0ull;
-    for (int r = 0; r < kk && tau != 0; ++r) tau = block_max(mine < tau ? mine : 0ull);
-    if (threadIdx.x == 0) shared.count = 0;
-    __syncthreads();
-    // keys are built only for scores that reach tau's score (a cheap float test first)
-    const uint32_t tu = (uint32_t)(tau >> 32);
-    const float tau_score = tau == 0 ? -INFINITY : __uint_as_float((tu & 0x80000000u) ? (tu & 0x7FFFFFFFu) : ~tu);
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-        const int j = local_of(e);
-        if (is(e, j) && v[e] >= tau_score) {
-            const uint64_t key = score_key(v[e], (uint32_t)(seg0 + j));
-            if (key >= tau) {
-                const uint32_t at = atomicAdd(&shared.count, 1u);
-                if (at < TOPK_MAX * EPT) list[at] = key;   // (more only where a score is NaN, which no key ranks)
-            }
-        }
-    }
-    __syncthreads();
-    const uint32_t n = min(shared.count, (uint32_t)(TOPK_MAX * EPT));
-    uint64_t prev = ~0ull;
-    for (int r = 0; r < kk; ++r) {
-        uint64_t best = 0;
-        for (uint32_t q = threadIdx.x; q < n; q += NT) {
-            const uint64_t key = list[q];
-            if (key < prev && key > best) best = key;
-        }
-        prev = block_max(best);
-        if (threadIdx.x == 0) dst[r] = prev;
-    }
-}
