@@ -99,36 +99,44 @@ k_topk_segments(const float* __restrict__ out, int64_t m, int kk, int nseg, uint
 
 // One workgroup per row: the best kk of the row's nseg*kk candidate keys, unpacked.  A launch of its own: merged by the workgroup
 // that finishes a row's last segment, behind fences, one row of 500k scores took 14.6 us when the two launches took 7.5 + 5.2.  (Without fences it
-// pays for one instance: k_forward_few.)
-template <int NT>
-__global__ void __launch_bounds__(NT)
+// pays for one instance: k_forward_few.)  Rows of any number of candidates: a lane keeps the best of its own, and when that one is given away its wavefront
+// looks through the lane's candidates once more.  (All lanes looking through theirs for each of the kk took 178 us for 45 344 candidates, 32 labels, this 49.)
+constexpr int MERGE_NT = 1024;
+__global__ void __launch_bounds__(MERGE_NT)
 k_topk_merge(const uint64_t* __restrict__ cand, int n, int kk, int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
-    __shared__ uint64_t red[2][NT / 64];
-    BlockMax<NT> block_max = {red, 0};
+    constexpr int AT_ONCE = 8;
+    __shared__ uint64_t red[2][MERGE_NT / 64];
+    BlockMax<MERGE_NT> block_max = {red, 0};
     const uint64_t* c = cand + (size_t)blockIdx.x * n;
-    constexpr int HELD = 8;   // candidates a lane keeps in registers; only very wide rows have more
-    uint64_t mine[HELD];
+    const int lane = threadIdx.x & 63;
+    uint64_t best = 0;
+    for (int q = (int)threadIdx.x; q < n; q += AT_ONCE * MERGE_NT) {
+        uint64_t key[AT_ONCE];
 #pragma unroll
-    for (int e = 0; e < HELD; ++e) mine[e] = e * NT + (int)threadIdx.x < n ? c[e * NT + threadIdx.x] : 0ull;
-    uint64_t prev = ~0ull;
+        for (int u = 0; u < AT_ONCE; ++u) key[u] = c[min(q + u * MERGE_NT, n - 1)];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) best = q + u * MERGE_NT < n && key[u] > best ? key[u] : best;
+    }
     for (int r = 0; r < kk; ++r) {
-        uint64_t best = 0;
-#pragma unroll
-        for (int e = 0; e < HELD; ++e)
-            if (mine[e] < prev && mine[e] > best) best = mine[e];
-        for (int q = HELD * NT + (int)threadIdx.x; q < n; q += NT) {
-            const uint64_t key = c[q];
-            if (key < prev && key > best) best = key;
-        }
-        prev = block_max(best);
+        const uint64_t prev = block_max(best);
         if ((int)threadIdx.x == r) {
             top_lab[(size_t)blockIdx.x * kk + r] = prev ? key_label(prev) : -1;   // fewer than kk labels are allowed
             top_val[(size_t)blockIdx.x * kk + r] = prev ? key_score(prev) : -INFINITY;
         }
+        const uint64_t given = __ballot(prev != 0 && best == prev);   // keys are distinct: one lane of the workgroup
+        if (given == 0) continue;
+        const int winner = __ffsll((unsigned long long)given) - 1;
+        uint64_t next = 0;
+        for (int q = (int)(threadIdx.x & ~63u) + winner + lane * MERGE_NT; q < n; q += 64 * MERGE_NT) {
+            const uint64_t key = c[q];
+            if (key < prev && key > next) next = key;
+        }
+        next = wave_max(next);
+        if (lane == winner) best = next;
     }
 }
 
-// Rows of few candidates, a wavefront each: no barriers.  (256 rows of 80, 10 labels: 8.1 us by a workgroup each and barriers, 4.8 so.)
+// Rows of few candidates, a wavefront each: no barriers.  (7 rows of 147, 1 label: 2.5 us by a workgroup each and a barrier a label, 1.7 so.)
 constexpr int MERGE_HELD = 4;
 __global__ void __launch_bounds__(256)
 k_topk_merge_few(const uint64_t* __restrict__ cand, int n, int b, int kk, int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
@@ -147,9 +155,10 @@ k_topk_merge_few(const uint64_t* __restrict__ cand, int n, int b, int kk, int32_
     top_val[(size_t)i * kk + lane] = best ? key_score(best) : -INFINITY;
 }
 
-// Rows of more, a workgroup each: its wavefronts find theirs, the first one the row's.  (1225 candidates, 5 labels: 4.1 us with a barrier a label, 3.6 so;
-// 256 rows of 410: 8.2 and 6.5; 7840, 32 labels: 56 and 32.)
-constexpr int MERGE_ROW_HELD = 8, MERGE_LONG_HELD = 16;
+// Rows of more, a workgroup each: its wavefronts find theirs, the first one the row's.  As few lanes, and as few candidates to a lane, as hold them: every wavefront of a
+// SIMD looks through its own for each label.  (us with a barrier a label and this: 1225 candidates, 5 labels 3.8 and 3.4; 256 rows of 410, 10 labels 7.4 and 5.3; 3720, 5 labels 5.8
+// and 4.0, with 1024 lanes of 16 candidates 7.0; 7840, 32 labels 31 and 20.)
+constexpr int MERGE_ROW_MOST = 16 * 1024;
 template <int NT, int HELD>
 __global__ void __launch_bounds__(NT)
 k_topk_merge_row(const uint64_t* __restrict__ cand, int n, int kk, int32_t* __restrict__ top_lab, float* __restrict__ top_val) {
@@ -220,12 +229,15 @@ usl_status usl_launch_topk_merge(usl_ctx* c, int nseg, int32_t b, int32_t kk, in
     const int n = nseg * kk;
     if (n <= MERGE_HELD * 64)
         hipLaunchKernelGGL(k_topk_merge_few, dim3((unsigned)((b + 3) / 4)), dim3(256), 0, c->stream, c->topk_cand, n, (int)b, (int)kk, top_lab, top_val);
-    else if (n <= MERGE_ROW_HELD * 256)
-        hipLaunchKernelGGL((k_topk_merge_row<256, MERGE_ROW_HELD>), dim3((unsigned)b), dim3(256), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
-    else if (n <= MERGE_LONG_HELD * 1024)
-        hipLaunchKernelGGL((k_topk_merge_row<1024, MERGE_LONG_HELD>), dim3((unsigned)b), dim3(1024), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
+#define USL_MERGE_ROW(NT, HELD) hipLaunchKernelGGL((k_topk_merge_row<NT, HELD>), dim3((unsigned)b), dim3(NT), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val)
+    else if (n <= 4 * 256) USL_MERGE_ROW(256, 4);
+    else if (n <= 8 * 256) USL_MERGE_ROW(256, 8);
+    else if (n <= 8 * 512) USL_MERGE_ROW(512, 8);
+    else if (n <= 16 * 512) USL_MERGE_ROW(512, 16);
+    else if (n <= MERGE_ROW_MOST) USL_MERGE_ROW(1024, 16);
+#undef USL_MERGE_ROW
     else
-        hipLaunchKernelGGL(k_topk_merge<1024>, dim3((unsigned)b), dim3(1024), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
+        hipLaunchKernelGGL(k_topk_merge, dim3((unsigned)b), dim3(MERGE_NT), 0, c->stream, c->topk_cand, n, (int)kk, top_lab, top_val);
     return usl_check_launch(c, "topk");
 }
 

@@ -2,7 +2,7 @@
 #pragma once
 #include "usl_internal.h"
 
-constexpr int TOPK_SHORT_MERGE = 8 * 256;   // candidates that a merge of 256 lanes holds in registers; more take it 1024
+constexpr int TOPK_SHORT_MERGE = 8 * 256;   // candidates that a merge of 256 lanes holds in registers; more take 512 or 1024
 constexpr int TOPK_SHORT_SEGMENT = 8 * 256;  // scores of a workgroup of the pass over them where rows are few
 constexpr int TOPK_MAX = 32;                 // largest kk
 
