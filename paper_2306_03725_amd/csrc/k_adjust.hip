@@ -5,8 +5,9 @@
 //   z <- z + bias[j];  not allowed: -infinity
 //
 // A workgroup takes a segment of one instance's scores into registers, all loads in flight at once, and counts the labels of its segment in the instance's
-// list: the list is short next to the scores, so every segment looks at all of it, and no pass has to sort it.  Bound by the stream of the scores:
-// 256 x 500k read and written, with a bias, a mask and lists of up to 500 labels each: 1.04 GB in 206 us, 5.1 TB/s, the rate of a large copy.
+// list: every segment looks at all of it, and no pass has to sort it.  Bound by the stream of the scores where lists are short next to a segment:
+// 256 x 500k read and written, with a bias, a mask and lists of up to 500 labels each: 1.04 GB in 206 us, 5.1 TB/s, the rate of a large copy.  Not so lists of thousands, whose
+// entries behind the first 1024 are read again by every segment, one after the other: 64 x 500k, lists of up to 1000 labels 57 us written and 51 as the 10 best, of up to 20 000 116 and 172.
 #include "k_topk.h"
 
 namespace {
@@ -32,7 +33,7 @@ struct Adjust {
 __device__ __forceinline__ int local_label(int e) { return ((e >> 2) * AD_NT + (int)threadIdx.x) * 4 + (e & 3); }
 
 // Four values from place j of lim, into registers.  full (the same for the workgroup): all of them are there; else those behind the end are the last one again.
-// (Never a load under a lane's condition: behind each of those the compiler waits.)
+// (Not a load under a lane's condition: behind each of those the compiler waits.)
 __device__ __forceinline__ void load_four(const float* p, int j, int lim, bool full, float* v) {
     if (full) {
         const f32x4 q = *reinterpret_cast<const f32x4*>(p + j);
@@ -73,7 +74,7 @@ struct Shown {
         };
 #pragma unroll
         for (int q = 0; q < HELD; ++q) one(held[q]);
-        for (int64_t p = HELD * AD_NT + (int)threadIdx.x; p < n; p += AD_NT) one(lab[p]);
+        for (int64_t p = HELD * AD_NT + (int)threadIdx.x; p < n; p += AD_NT) one(lab[p]);   // (each is waited for, and what was asked for before it)
     }
 };
 

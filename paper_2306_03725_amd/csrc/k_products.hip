@@ -587,7 +587,7 @@ Launch choose(const usl_ctx* c, const Layout& L, int b, ProductKind kind, int mo
         const double waits = !thin ? 1.0 : !backward ? 1.1 : kern.LPT > 1 ? 1.3 : 1.0;
         const double gather = (double)gpb * lanes * kern.K * (L.halves ? 2 : 1) / reads_per_clk * waits;
         const double more = copy > gather ? copy : gather, less = copy > gather ? gather : copy;
-        const double load = (double)labels * c->k * (4.0 + (backward ? 4.0 : es)) / 7.0;
+        const double load = (double)labels * c->k * (4.0 + (backward ? 4.0 : es)) / 7.0;   // (values in 4 bits count as others do; the choice was not measured with less)
         const double tiles = (double)((gpb + tg.tile_rows - 1) / tg.tile_rows) * (L.halves ? 2 : 1);
         const double latency = (double)gpb * ((labels + kern.NT - 1) / kern.NT) * kern.K * (L.halves ? 2 : 1) / (unit == 16 ? 4 : 8) * 200.0;
         double busy = per_cu * (more + (tg.nbuf == 2 || together > 1.5 ? 0.5 : 1.0) * less);
@@ -799,12 +799,13 @@ FewShape few_shape(const usl_ctx* c, const Layout& L, int kk) {
 // Prediction of one instance: the best labels from the forward kernel, or from kernels over its scores?  The forward kernel's workgroups look for theirs when
 // all wavefronts are done, 3 us of chains of maxima for 5 labels, and where two of 16 wavefronts share a compute unit or many labels are asked for their candidates take longer to
 // merge; the other way costs a launch and a pass of 6 us over scores in the cache, and 1 us of forward less.  usl_predict, from forward and with the pass, us (captured graphs):
-// smaller workgroups: m = 5000, d = 64, k = 8, 5 labels 8.5 and 11.2, 32 labels 31.1 and 41.8; m = 60 867, d = 1344, k = 16, 5 labels 11.7 and 12.0, not so 10 labels 18.9 and 18.0, 32 labels 76.8 and
-// 42.9; m = 49k, d = 1762, k = 32, 5 labels 12.9 and 14.5, not so 8 labels 19.2 and 18.1; m = 100k, d = 600, k = 8, 5 labels 9.6 and 11.9, not so 16 labels 27.5 and 24.6; m = 262k, d = 25k, k = 8, 32
-// labels (8192 candidates and 4096) 50.7 and 57.8;
-// one of 16 wavefronts to a compute unit: m = 500k, d = 32k, k = 32, 5 labels 28.6 and 30.8, 32 labels 70.0 and 74.7; m = 114k, d = 34k, k = 32, 5 labels 12.7 and 14.4 (32 labels 54.7 and 45.8);
-// not so two of them: m = 225 711, d = 118, k = 13, 5 labels 22.0 and 18.0; m = 109 071, d = 7213, k = 32 17.8 and 15.9; m = 720 436, d = 2151, k = 13 33.1 and 29.7 (m = 1.02M, d = 2473, k = 8 24.2 and 25.7);
-// three turns: m = 1.27M, d = 11k, k = 32, 5 labels 63.7 and 68.4, 32 labels 145 and 156; m = 1.32M, d = 561, k = 56, bfloat16 95.3 and 99.6 (m = 1.34M, d = 11k, k = 3 24.5 and 23.6).
+// smaller workgroups: m = 5000, d = 64, k = 8, 5 labels 8.8 and 10.0 (32 labels 31.5 and 29.8); m = 60 867, d = 1344, k = 16, 5 labels 10.2 and 10.7, not so 10 labels 16.5 and 16.2, 32 labels 50.1 and
+// 34.9; m = 49k, d = 1762, k = 32, 5 labels 13.0 and 12.7, not so 8 labels 16.2 and 15.2; m = 100k, d = 600, k = 8, 5 labels 9.7 and 10.7, not so 16 labels 22.6 and 21.2; m = 262k, d = 25k, k = 8, 32
+// labels (8192 candidates and 4096) 40.0 and 42.1;
+// one of 16 wavefronts to a compute unit: m = 500k, d = 32k, k = 32, 5 labels 30.5 and 32.3, 32 labels 61.4 and 64.7; m = 114k, d = 34k, k = 32, 5 labels 13.0 and 14.4 (32 labels 44.3 and 40.1);
+// not so two of them: m = 225 711, d = 118, k = 13, 5 labels 20.4 and 17.5; m = 109 071, d = 7213, k = 32 16.4 and 15.3; m = 720 436, d = 2151, k = 13 31.6 and 29.4 (m = 1.02M, d = 2473, k = 8 23.3 and 24.7);
+// three turns: m = 1.27M, d = 11k, k = 32, 5 labels 61.9 and 65.4, 32 labels 111 and 126; m = 1.32M, d = 561, k = 56, bfloat16 94.0 and 98.0 (m = 1.34M, d = 11k, k = 3 22.7 and 22.3).
+// (In brackets where the rule is on the slower side, 10 % at most.)
 bool best_from_forward(const usl_ctx* c, const FewShape& f, int kk) {
     if (f.nw < 16) {
         const int64_t n = (int64_t)f.grid * kk, by_pass = (c->m + TOPK_SHORT_SEGMENT - 1) / TOPK_SHORT_SEGMENT * kk;   // candidates
@@ -814,13 +815,14 @@ bool best_from_forward(const usl_ctx* c, const FewShape& f, int kk) {
 }
 
 // ... and who merges the workgroups' candidates: the one that comes last, or a launch of its own?  The last one has waited for the others at the count, which
-// takes 11.5 ns of each, and saves a launch; a launch of more than TOPK_SHORT_MERGE candidates takes 3 to 6 us longer.  So it is the last one with few workgroups (the more, the
+// takes 11.5 ns of each, and saves a launch; a launch takes the longer the more candidates there are.  So it is the last one with few workgroups (the more, the
 // more labels are asked for), with many candidates, and where the stream of idx and W lasts so long that the workgroups come in spread out.  usl_predict, last workgroup and
-// launch, from captured graphs | call by call, us: 47 workgroups, 1 label 5.55 and 5.40 | 6.2 and 8.8; 79, 3 labels 7.5 and 7.3 | 7.6 and 8.4; 79, 10 labels 13.4 and 14.1 | 13.2 and 14.1;
-// not so 118, 1 label 6.3 and 5.4 | 7.0 and 8.8; 157, 5 labels 9.9 and 9.3 | 9.9 and 9.9; 254, 2 labels 8.6 and 6.5 | 8.6 and 8.3; 256 of 8 wavefronts (m = 131k, d = 25k, k = 16), 5 labels 12.8 and
-// 10.8 | 12.7 and 11.0; 256 of 16 wavefronts with 29 MB (m = 114k, d = 34k, k = 32), 5 labels 14.5 and 13.0 | 14.3 and 13.1, 10 labels 19.7 and 22.5 | 19.5 and 22.4; with 45 MB (m = 175k, d = 33k) 5 labels
-// 19.9 and 19.7 | 18.4 and 18.7; with 128 MB (m = 500k, d = 32k) 30.0 and 29.8 | 30.1 and 30.0, 10 labels 33.9 and 37.4 | 35.3 and 39.4.  (Two workgroups to a compute unit: their candidates, twice as many,
-// come late; m = 1.34M, d = 11k, k = 3 25.1 us with a launch for the merge, 26.1 without.)
+// launch, from captured graphs | call by call, us: 47 workgroups, 1 label 5.6 and 5.7 | 5.4 and 7.1; 79, 3 labels 7.7 and 6.7 | 7.4 and 7.2; 79, 10 labels 13.5 and 12.2 | 13.2 and 12.1;
+// not so 118, 1 label 6.4 and 5.8 | 6.2 and 7.1; 157, 5 labels 10.2 and 8.7 | 9.9 and 8.6; 254, 2 labels 8.9 and 6.6 | 8.6 and 7.2; 256 of 8 wavefronts (m = 131k, d = 25k, k = 16), 5 labels 13.0 and
+// 10.8 | 12.7 and 10.7; 256 of 16 wavefronts with 29 MB (m = 114k, d = 34k, k = 32), 5 labels 14.5 and 12.5 | 14.1 and 12.4, 10 labels 19.8 and 17.9 | 19.4 and 17.7; with 45 MB (m = 175k, d = 33k) 5 labels
+// 20.3 and 20.1 | 19.8 and 19.4; with 128 MB (m = 500k, d = 32k) 28.9 and 28.2 | 28.5 and 27.8, 10 labels 34.3 and 35.2 | 33.8 and 34.8.  The rule dates from a merge that took 3 to 6 us longer
+// for more than TOPK_SHORT_MERGE candidates; with the present one a launch would be the better choice in several of these, by 1 to 2 us.  (Two workgroups to a compute unit: their candidates, twice as many,
+// come late; m = 1.34M, d = 11k, k = 3 25.1 us with a launch for the merge, 26.1 without, measured with that merge.)
 bool last_one_merges(const usl_ctx* c, const FewShape& f, int kk) {
     const int64_t n = (int64_t)f.grid * kk, stream = c->m * c->k * (c->storage == USL_F32 ? 8 : 6);
     if (f.grid > (unsigned)c->num_cu || n > (int64_t)FEW_HELD * f.nw * 64) return false;
