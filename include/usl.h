@@ -299,6 +299,66 @@ usl_status usl_adjust_scores(usl_ctx* ctx, const float* out, const usl_adjustmen
 usl_status usl_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk,
                              int32_t* top_lab, float* top_val);
 
+/* ---- In front of the layer: the gated block that widens a trunk's output e to the activations x, and its products in 8-bit integers ----
+ * (The paper feeds the layer from one dense "intermediate" layer of 16 to 65 thousand units; the block has two, the second gated by the first.)
+ * e [b][w] storage type, the trunk's output; V_gate, V_up [d][w] storage type.  1 <= w <= 65536, d <= 2^20 (else USL_ESHAPE).
+ * act: what the gate goes through, USL_SILU a / (1 + exp(-a)) or USL_GELU a * Phi(a), Phi the standard normal distribution's function. */
+typedef enum { USL_SILU = 0, USL_GELU = 1 } usl_act;
+
+/*   gate[i][c] = sum_t e[i][t] * V_gate[c][t],  up[i][c] = sum_t e[i][t] * V_up[c][t],  x[i][c] = act(gate[i][c]) * up[i][c]
+ * x [b][d] storage type; gate, up [b][d] storage type, results for usl_gated_block_backward, each may be NULL.  Sums and act are float32 (of sums that
+ * have not been rounded), and every result is rounded once.  None of the results may be an input or another result. */
+usl_status usl_gated_block(usl_ctx* ctx, const void* e, const void* V_gate, const void* V_up, int32_t w, int32_t act, void* x, void* gate,
+                           void* up, int32_t b);
+
+/* Its backward pass, from the gradient by x that usl_backward_input, usl_backward, usl_train_step and usl_layer_norm_backward return:
+ *   G_gate = grad_x * up * act'(gate),  G_up = grad_x * act(gate)
+ *   grad_e = G_gate V_gate + G_up V_up [b][w],  grad_V_gate = G_gate^T e,  grad_V_up = G_up^T e [d][w]
+ * e, V_gate, V_up as the forward call had them, gate and up as it left them.  grad_x and the results are float32, overwritten; each result may be
+ * NULL, and none may be an input or another result.  Everything is computed in float32.  Where e, a matrix or G holds an infinity, the sums that it enters
+ * are infinite or NaN.  Sums are taken in a fixed order: equal calls give equal bits.  Scratch is sized by w: a larger w than before reallocates and waits. */
+usl_status usl_gated_block_backward(usl_ctx* ctx, const float* grad_x, const void* e, const void* V_gate, const void* V_up, const void* gate,
+                                    const void* up, int32_t w, int32_t act, float* grad_e, float* grad_V_gate, float* grad_V_up, int32_t b);
+
+/* Rows in 8-bit integers with a scale each (a row of e: a token; a row of a matrix: a channel).  rows [n][w] storage type, codes [n][w] int8, scales [n]:
+ *   scale = max(largest magnitude of the row / 127, 2^-126),  code = value / scale to the nearest integer, halves to the even one, within -127..127
+ * Both quotients are rounded to float32.  A row with an infinity or NaN has NaN as its scale, and codes 0.  1 <= n < 2^31. */
+usl_status usl_quantize_i8(usl_ctx* ctx, const void* rows, int64_t n, int32_t w, int8_t* codes, float* scales);
+
+/* One projection in such numbers:  h[i][c] = (sum_t e_codes[i][t] * V_codes[c][t]) * (e_scales[i] * V_scales[c])
+ * h [b][d] storage type; e_codes [b][w], e_scales [b], V_codes [d][w], V_scales [d].  The sum is exact, and h rounded once from float32. */
+usl_status usl_project_i8(usl_ctx* ctx, const int8_t* e_codes, const float* e_scales, const int8_t* V_codes, const float* V_scales, int32_t w,
+                          void* h, int32_t b);
+
+/* usl_gated_block with both projections in such numbers. */
+usl_status usl_gated_block_i8(usl_ctx* ctx, const int8_t* e_codes, const float* e_scales, const int8_t* gate_codes, const float* gate_scales,
+                              const int8_t* up_codes, const float* up_scales, int32_t w, int32_t act, void* x, int32_t b);
+
+/* ---- What the layer learns from beside label lists: a softmax over all its labels against short lists of them ----
+ * The lists are CSR as the targets are: off [b+1] int64, lab [off[b]] int32, and a value (or several) for each entry.  An entry counts if its label
+ * lies in [0, m), that label's score is above -infinity (so a label that usl_adjust_scores has masked is in no distribution and in no list) and, for a
+ * teacher, so is its logit.  Several entries of one label count one by one.  A row with no entry that counts adds nothing to the loss, and its g is zero.  A row
+ * with one whose scores hold NaN or +infinity has NaN.  out, g [b][m]; g may be out, or NULL (the loss alone).  loss: one float32 in device memory.  out, loss, g
+ * and logp are overwritten only where they are results.  Sums are taken in a fixed order: equal calls give equal bits. */
+
+/* Distillation from a teacher's best labels and their logits (tea_logit float32).  T = temperature, finite and > 0:
+ *   q[i] = softmax of out[i] / T over all labels,  p[i] = softmax of the logits / T over the entries of row i that count
+ *   loss = scale * T^2 * sum_i sum_e p[e] * (log p[e] - log q[i][tea_lab[e]])
+ *   g[i][j] = scale * T * (q[i][j] - sum of p[e] over the entries of label j) */
+usl_status usl_distill_loss_grad(usl_ctx* ctx, const float* out, const int64_t* tea_off, const int32_t* tea_lab, const float* tea_logit,
+                                 float temperature, float scale, float* g, float* loss, int32_t b);
+
+/* A clipped policy objective: the layer is a policy that answers instance i with labels, act_lab its answers.  old_logp: their log-probabilities under the
+ * policy that gave them, ref_logp: under a reference policy, advantage: how much better than expected they were; all float32, one for each entry.
+ *   logp[e] = log softmax(out[i])[act_lab[e]],  r = exp(logp - old_logp),  u = ref_logp - logp
+ *   loss = scale * sum_e [ -min(r * advantage, clamp(r, 1 - clip_low, 1 + clip_high) * advantage) + beta * (exp(u) - u - 1) ]
+ *   g = its gradient by out.  (Where both sides of the minimum are equal, that of the first.)
+ * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0, all finite; ref_logp may be NULL if beta is 0.  logp: float32, one for each entry, a result (-infinity for an entry that does not
+ * count), or NULL; it must not be an input.  With g NULL this is also how old_logp and ref_logp are made. */
+usl_status usl_policy_loss_grad(usl_ctx* ctx, const float* out, const int64_t* act_off, const int32_t* act_lab, const float* old_logp,
+                                const float* ref_logp, const float* advantage, float clip_low, float clip_high, float beta, float scale,
+                                float* g, float* logp, float* loss, int32_t b);
+
 /* Debug check of the uniform-sparsity invariant (Section 3.2): counts rows of idx that hold a
  * value outside [0, d) or the same column twice.  n_bad_host: host pointer; the call waits. */
 usl_status usl_validate_indices(usl_ctx* ctx, const int32_t* idx, int64_t* n_bad_host);

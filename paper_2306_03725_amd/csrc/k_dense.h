@@ -1,0 +1,218 @@
+// Device code of the dense products around the layer: out[n][m] = sum over kk of A[m][kk] * B[n][kk] on the matrix cores, both operands staged through
+// LDS.  m is the axis along which the output is contiguous: a lane of a 16 x 16 tile holds four neighbours in m of one n.
+//
+// K is walked in steps.  An operand's tile of a step is either KC (its rows are m or n, with the step's values of K side by side) or KO (its rows are
+// values of K, as its memory has them: the transpose is made by the reads, ds_read_b64_tr_b16 for 16-bit numbers).  A fragment is 16 bytes a lane in both
+// cases: lane l has row l % 16 and the bytes of group l / 16 of 64 bytes of K.
+//
+// Tiles go from memory to LDS without registers between (buffer_load_dwordx4 ... lds: a wavefront's 64 x 16 bytes land one behind the other), so
+// which 16 bytes a lane asks for decides what lies where: groups of 16 bytes of a row are permuted by a key of the row, by which the lanes whose reads meet
+// (k_lanes.h) touch every bank once.  Rows behind the end are the last row again (their results are dropped), groups behind the end of K are asked for out of
+// the buffer's range and arrive as zeros.
+#pragma once
+#include "usl_internal.h"
+
+namespace dense {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(1)));   // 16 bytes from any address
+
+struct bf16 { uint16_t bits; };
+
+// A step of 64 bytes of K on the matrix cores
+template <typename T> struct Core;
+template <> struct Core<bf16> {
+    using Acc = f32x4;
+    static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Core<float> {   // the j-th of four products takes value j of every lane: K in another order, the same for both operands
+    using Acc = f32x4;
+    static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct Core<int8_t> {
+    using Acc = i32x4;
+    static __device__ __forceinline__ Acc mul(i32x4 a, i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// What a lane asks a buffer for when it wants zeros: behind the end that the buffer below claims
+constexpr uint32_t NOWHERE = 0x80000000u;
+
+// A buffer from p on: every offset that is used lies inside the caller's memory or is NOWHERE.
+__device__ __forceinline__ i32x4 buffer_at(const void* p) {
+    const uint64_t a = (uint64_t)p;
+    i32x4 r;
+    r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    r.y = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF);
+    r.z = 0x7FFFFFF0;
+    r.w = 0x00020000;
+    return r;
+}
+// 16 bytes a lane from buffer + off to LDS, at `to` + 16 * lane.  M0 is written without the compiler's knowledge: the kernels here have no other use of it.
+__device__ __forceinline__ void to_lds(uint32_t to, const i32x4& buffer, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(off), "s"(buffer) : "memory");
+}
+__device__ __forceinline__ void landed() {   // what this wavefront asked for is there; behind a barrier, what all did
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// The n values (bytes: n * sizeof(T)) from p on, zeros behind them.  n may be 0 or less; 16 bytes at most.
+template <typename T>
+__device__ __forceinline__ i32x4 sixteen(const char* p, int bytes) {
+    if (bytes >= 16) return *reinterpret_cast<const i32x4_any*>(p);
+    i32x4 r = {0, 0, 0, 0};
+    T v[16 / sizeof(T)];
+    __builtin_memcpy(v, &r, 16);
+#pragma unroll
+    for (int j = 0; j < (int)(16 / sizeof(T)); ++j)
+        if ((j + 1) * (int)sizeof(T) <= bytes) v[j] = reinterpret_cast<const T*>(p)[j];
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+
+// ---- KC: ROWS rows of KB (128 or 64) bytes of K
+// The row of a tile that fragment f's row i is.  SPREAD fragments side by side: a lane's four neighbours of each of them are 4 * SPREAD neighbours.
+template <int SPREAD>
+__device__ __forceinline__ int frag_row(int f, int i) {
+    return SPREAD == 1 ? f * 16 + i : (f / SPREAD) * (16 * SPREAD) + (i >> 2) * (4 * SPREAD) + (f % SPREAD) * 4 + (i & 3);
+}
+// Which group of 16 bytes of a row lies at place p of it (and the other way round).  The 16 lanes that meet read rows i = 0-3 and 12-15 of a fragment at one
+// group, rows 4-11 at the next one (k_lanes.h).  128 bytes: two rows cover the banks, 8 rows' keys have to differ.  64: four rows.
+template <int KB, int SPREAD>
+__device__ __forceinline__ int place_of(int row, int p) {
+    const int q = SPREAD == 1 ? row >> 2 : row / (4 * SPREAD);   // i >> 2 of the fragment's row
+    if (KB == 128) return p ^ ((row & 3) | (q & 1) << 2);
+    return p ^ ((q >> 1 & 1) | ((q ^ q >> 1) & 1) << 1);
+}
+template <int ROWS, int KB, int SPREAD, int WAVES>
+struct StageKC {
+    static constexpr int AT_ONCE = 1024 / KB, LOADS = ROWS / AT_ONCE / WAVES;   // rows of a wavefront's load
+    static_assert(LOADS * AT_ONCE * WAVES == ROWS, "rows are dealt evenly");
+    static constexpr int BYTES = ROWS * KB;
+    static __device__ __forceinline__ int row_of(int t) { return (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE + (int)(threadIdx.x & 63) / (KB / 16); }
+    static __device__ __forceinline__ int group_of(int t) { return place_of<KB, SPREAD>(row_of(t), (int)(threadIdx.x & 63) % (KB / 16)); }
+    // from: row 0 of the tile at this step's first byte; rows: how many there are; left: bytes of K from here to the end (multiples of 16, as from's address)
+    static __device__ __forceinline__ void direct(uint32_t lds, const char* from, int rows, uint32_t pitch, int left) {
+        const i32x4 buffer = buffer_at(from);
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int g = group_of(t) * 16;
+            const uint32_t off = (uint32_t)min(row_of(t), rows - 1) * pitch + (uint32_t)g;
+            to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, g < left ? off : NOWHERE);
+        }
+    }
+    // the same through registers, for rows at any address: fetch, then (behind the step before) put
+    template <typename T>
+    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int rows, uint32_t pitch, int left) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int g = group_of(t) * 16;
+            const char* p = from + (size_t)min(row_of(t), rows - 1) * pitch + g;
+            held[t] = left >= KB ? *reinterpret_cast<const i32x4_any*>(p) : sixteen<T>(p, left - g);
+        }
+    }
+    static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + (t * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16) = held[t];
+    }
+    // fragment f's 16 bytes of this lane, 64-byte part h of the step; row0: the wavefront's first row of the tile
+    static __device__ __forceinline__ i32x4 frag(const char* lds, int row0, int f, int h) {
+        const int l = (int)(threadIdx.x & 63), row = row0 + frag_row<SPREAD>(f, l & 15);
+        return *reinterpret_cast<const i32x4*>(lds + row * KB + place_of<KB, SPREAD>(row, h * 4 + (l >> 4)) * 16);
+    }
+};
+
+// ---- KO: rows of COLS values, a row for each value of K in a step of 64 bytes of K
+template <typename T, int COLS, int WAVES>
+struct StageKO {
+    static constexpr int DEPTH = 64 / (int)sizeof(T), ROW = COLS * (int)sizeof(T), GROUPS = ROW / 16, AT_ONCE = 64 / GROUPS, LOADS = DEPTH / AT_ONCE / WAVES;
+    static_assert(GROUPS <= 64 && LOADS * AT_ONCE * WAVES == DEPTH, "rows are dealt evenly");
+    static constexpr int BYTES = DEPTH * ROW;
+    // 16-bit: 32 lanes read 32 bytes of the rows k = 0-3 and 8-11 (then 4-7 and 12-15, ...): blocks of 32 bytes are permuted by a key that differs between those.
+    // 32-bit: 64 lanes read 64 bytes of the rows j, 4 + j, 8 + j, 12 + j: blocks of 64 bytes by k / 4.
+    static __device__ __forceinline__ int group_at(int k, int p) {
+        if (sizeof(T) == 2) return p ^ (((k & 3) | (k >> 3 & 1) << 2) << 1 & (GROUPS - 1));
+        return p ^ ((k >> 2 & 3) << 2 & (GROUPS - 1));
+    }
+    static __device__ __forceinline__ int row_of(int t) { return (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE + (int)(threadIdx.x & 63) / GROUPS; }
+    static __device__ __forceinline__ int group_of(int t) { return group_at(row_of(t), (int)(threadIdx.x & 63) % GROUPS); }
+    // from: the tile's first column in the step's first row; depth: rows of K from here to the end; width: bytes from the first column to the end of a row
+    static __device__ __forceinline__ void direct(uint32_t lds, const char* from, int depth, size_t pitch, int width) {
+        const i32x4 buffer = buffer_at(from);
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int g = group_of(t) * 16, k = row_of(t);
+            to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, k < depth && g < width ? (uint32_t)k * (uint32_t)pitch + (uint32_t)g : NOWHERE);
+        }
+    }
+    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int depth, size_t pitch, int width) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int g = group_of(t) * 16, k = row_of(t);
+            held[t] = sixteen<T>(from + (size_t)k * pitch + g, k < depth ? width - g : 0);
+        }
+    }
+    static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + (t * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16) = held[t];
+    }
+    // fragment of the 16 columns from col (a multiple of 16) on
+    static __device__ __forceinline__ i32x4 frag(const char* lds, int col) {
+        const int l = (int)(threadIdx.x & 63), g = l >> 4;
+        if (sizeof(T) == 2) {
+            // 16 lanes give the addresses of 4 x 16 numbers, four lanes a row, and receive a column each
+            typedef __attribute__((address_space(3))) i16x4 lds4;
+            const int k = 8 * g + ((l & 15) >> 2), at = col * 2 + (l & 3) * 8;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + k * ROW + group_at(k, at >> 4) * 16 + (at & 8)));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + (k + 4) * ROW + group_at(k + 4, at >> 4) * 16 + (at & 8)));
+            return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        i32x4 r;
+        const int at = (col + (l & 15)) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = 4 * g + j;
+            r[j] = *reinterpret_cast<const int*>(lds + k * ROW + group_at(k, at >> 4) * 16 + (at & 15));
+        }
+        return r;
+    }
+};
+
+// ---- the block's activations
+template <int ACT>   // 0: a / (1 + exp(-a)); 1: a * Phi(a), the normal distribution's function
+__device__ __forceinline__ float act_of(float a) {
+    if (ACT == 0) return a / (1.f + expf(-a));
+    return 0.5f * a * (1.f + erff(a * 0.70710678f));
+}
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float a, float& value, float& slope) {
+    if (ACT == 0) {
+        const float p = 1.f / (1.f + expf(-a));
+        value = a * p;
+        slope = p * (1.f + a * (1.f - p));
+    } else {
+        const float phi = 0.5f * (1.f + erff(a * 0.70710678f));
+        value = a * phi;
+        slope = phi + a * 0.39894228f * expf(-0.5f * a * a);
+    }
+}
+
+template <typename T> __device__ __forceinline__ T narrow(float v);
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 narrow<bf16>(float v) { return bf16{usl_f32_to_bf16(v)}; }
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16 v) { return usl_bf16_to_f32(v.bits); }
+
+}  // namespace dense

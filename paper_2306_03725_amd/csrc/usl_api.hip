@@ -32,7 +32,7 @@ extern "C" usl_status usl_destroy(usl_ctx* c) {
     if (c->device >= 0) {
         void* bufs[] = {c->bce_partials, c->sel_hist, c->prune_flags, c->tie_counts, c->counter64,
                         c->csc_ptr, c->csc_cursor, c->csc_order, c->csc_slot, c->csc_w, c->gT, c->gxT, c->nz_flags,
-                        c->slot_order, c->topk_cand, c->sub_idx, c->sub_W, c->predict_out, c->norm_part, c->gw_part,
+                        c->slot_order, c->topk_cand, c->sub_idx, c->sub_W, c->predict_out, c->norm_part, c->gated_scratch, c->list_part, c->gw_part,
                         c->nz_state, c->nz_bits, c->nz_lab, c->nz_val, c->idx_print, c->xi, c->xr, c->tgt_bits, c->small_sums, c->small_order};
         (void)hipStreamSynchronize(c->stream);
         for (void* p : bufs)
@@ -581,6 +581,126 @@ extern "C" usl_status usl_topk_adjusted(usl_ctx* c, const float* out, const usl_
         USL_FAIL(c, USL_ESHAPE, "kk = %d, this build takes at most min(m, %d)", kk, usl_topk_max());
     USL_TRY(usl_prepare_device(c));
     return usl_launch_topk_adjusted(c, out, adj, b, kk, top_lab, top_val);
+}
+
+// ---- in front of the layer, and losses against short lists
+
+static usl_status check_block(usl_ctx* c, int32_t w) {
+    if (w < 1) USL_FAIL(c, USL_EINVAL, "w = %d < 1", w);
+    if (w > 65536) USL_FAIL(c, USL_ESHAPE, "w = %d, this build takes at most 65536", w);
+    if (c->d > 1 << 20) USL_FAIL(c, USL_ESHAPE, "d = %d, the dense calls take at most 2^20", c->d);
+    return USL_OK;
+}
+static usl_status check_act(usl_ctx* c, int32_t act) {
+    if (act != USL_SILU && act != USL_GELU) USL_FAIL(c, USL_EINVAL, "act %d is neither USL_SILU nor USL_GELU", act);
+    return USL_OK;
+}
+// No result is an input or another result; NULLs are passed over
+static usl_status check_apart(usl_ctx* c, const void* const* results, int n_results, const void* const* inputs, int n_inputs) {
+    for (int r = 0; r < n_results; ++r) {
+        if (!results[r]) continue;
+        for (int i = 0; i < n_inputs; ++i)
+            if (results[r] == inputs[i]) USL_FAIL(c, USL_EINVAL, "a result is an input");
+        for (int q = 0; q < r; ++q)
+            if (results[r] == results[q]) USL_FAIL(c, USL_EINVAL, "a result is another result");
+    }
+    return USL_OK;
+}
+
+extern "C" usl_status usl_gated_block(usl_ctx* c, const void* e, const void* V_gate, const void* V_up, int32_t w, int32_t act, void* x, void* gate,
+                                      void* up, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(e); NEED(V_gate); NEED(V_up); NEED(x);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_block(c, w));
+    USL_TRY(check_act(c, act));
+    const void *results[] = {x, gate, up}, *inputs[] = {e, V_gate, V_up};
+    USL_TRY(check_apart(c, results, 3, inputs, 3));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_gated(c, e, V_gate, V_up, w, act, x, gate, up, b);
+}
+
+extern "C" usl_status usl_gated_block_backward(usl_ctx* c, const float* grad_x, const void* e, const void* V_gate, const void* V_up, const void* gate,
+                                               const void* up, int32_t w, int32_t act, float* grad_e, float* grad_V_gate, float* grad_V_up, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(grad_x); NEED(e); NEED(V_gate); NEED(V_up); NEED(gate); NEED(up);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_block(c, w));
+    USL_TRY(check_act(c, act));
+    const void *results[] = {grad_e, grad_V_gate, grad_V_up}, *inputs[] = {grad_x, e, V_gate, V_up, gate, up};
+    USL_TRY(check_apart(c, results, 3, inputs, 6));
+    if (!grad_e && !grad_V_gate && !grad_V_up) return USL_OK;
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_gated_backward(c, grad_x, e, V_gate, V_up, gate, up, w, act, grad_e, grad_V_gate, grad_V_up, b);
+}
+
+extern "C" usl_status usl_quantize_i8(usl_ctx* c, const void* rows, int64_t n, int32_t w, int8_t* codes, float* scales) {
+    if (!c) return USL_EINVAL;
+    NEED(rows); NEED(codes); NEED(scales);
+    if (n < 1) USL_FAIL(c, USL_EINVAL, "n = %lld < 1", (long long)n);
+    if (n > 0x7FFFFFFFll) USL_FAIL(c, USL_ESHAPE, "n = %lld is too large", (long long)n);
+    USL_TRY(check_block(c, w));
+    const void *results[] = {codes, scales}, *inputs[] = {rows};
+    USL_TRY(check_apart(c, results, 2, inputs, 1));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_quantize_i8(c, rows, n, w, codes, scales);
+}
+
+extern "C" usl_status usl_project_i8(usl_ctx* c, const int8_t* e_codes, const float* e_scales, const int8_t* V_codes, const float* V_scales, int32_t w,
+                                     void* h, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(e_codes); NEED(e_scales); NEED(V_codes); NEED(V_scales); NEED(h);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_block(c, w));
+    const void *results[] = {h}, *inputs[] = {e_codes, e_scales, V_codes, V_scales};
+    USL_TRY(check_apart(c, results, 1, inputs, 4));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_dense_i8(c, e_codes, e_scales, V_codes, V_scales, nullptr, nullptr, w, USL_SILU, h, b);
+}
+
+extern "C" usl_status usl_gated_block_i8(usl_ctx* c, const int8_t* e_codes, const float* e_scales, const int8_t* gate_codes, const float* gate_scales,
+                                         const int8_t* up_codes, const float* up_scales, int32_t w, int32_t act, void* x, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(e_codes); NEED(e_scales); NEED(gate_codes); NEED(gate_scales); NEED(up_codes); NEED(up_scales); NEED(x);
+    USL_TRY(check_batch(c, b));
+    USL_TRY(check_block(c, w));
+    USL_TRY(check_act(c, act));
+    const void *results[] = {x}, *inputs[] = {e_codes, e_scales, gate_codes, gate_scales, up_codes, up_scales};
+    USL_TRY(check_apart(c, results, 1, inputs, 6));
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_dense_i8(c, e_codes, e_scales, gate_codes, gate_scales, up_codes, up_scales, w, act, x, b);
+}
+
+extern "C" usl_status usl_distill_loss_grad(usl_ctx* c, const float* out, const int64_t* tea_off, const int32_t* tea_lab, const float* tea_logit,
+                                            float temperature, float scale, float* g, float* loss, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(out); NEED(tea_off); NEED(tea_lab); NEED(tea_logit); NEED(loss);
+    if (!(temperature > 0.f) || isinf(temperature) || isinf(1.f / temperature)) USL_FAIL(c, USL_EINVAL, "temperature must be finite and > 0, and so must its reciprocal");
+    if (!(scale == scale) || isinf(scale)) USL_FAIL(c, USL_EINVAL, "scale is not finite");
+    USL_TRY(check_batch(c, b));
+    const void *results[] = {loss, g}, *inputs[] = {tea_off, tea_lab, tea_logit};
+    USL_TRY(check_apart(c, results, 2, inputs, 3));
+    if ((const void*)loss == (const void*)out) USL_FAIL(c, USL_EINVAL, "loss is an input");
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_distill(c, out, tea_off, tea_lab, tea_logit, temperature, scale, g, loss, b);
+}
+
+extern "C" usl_status usl_policy_loss_grad(usl_ctx* c, const float* out, const int64_t* act_off, const int32_t* act_lab, const float* old_logp,
+                                           const float* ref_logp, const float* advantage, float clip_low, float clip_high, float beta, float scale,
+                                           float* g, float* logp, float* loss, int32_t b) {
+    if (!c) return USL_EINVAL;
+    NEED(out); NEED(act_off); NEED(act_lab); NEED(old_logp); NEED(advantage); NEED(loss);
+    if (!(clip_low >= 0.f && clip_low <= 1.f)) USL_FAIL(c, USL_EINVAL, "clip_low must lie in [0, 1]");
+    if (!(clip_high >= 0.f) || isinf(clip_high)) USL_FAIL(c, USL_EINVAL, "clip_high must be finite and >= 0");
+    if (!(beta >= 0.f) || isinf(beta)) USL_FAIL(c, USL_EINVAL, "beta must be finite and >= 0");
+    if (beta > 0.f && !ref_logp) USL_FAIL(c, USL_EINVAL, "beta > 0 needs ref_logp");
+    if (!(scale == scale) || isinf(scale)) USL_FAIL(c, USL_EINVAL, "scale is not finite");
+    USL_TRY(check_batch(c, b));
+    const void *results[] = {loss, g, logp}, *inputs[] = {act_off, act_lab, old_logp, ref_logp, advantage};
+    USL_TRY(check_apart(c, results, 3, inputs, 5));
+    if ((const void*)loss == (const void*)out || (const void*)logp == (const void*)out) USL_FAIL(c, USL_EINVAL, "a result is an input");
+    USL_TRY(usl_prepare_device(c));
+    return usl_launch_policy(c, out, act_off, act_lab, old_logp, beta > 0.f ? ref_logp : nullptr, advantage, clip_low, clip_high, beta, scale, g, logp, loss, b);
 }
 
 extern "C" usl_status usl_check(usl_ctx* c) {

@@ -67,6 +67,8 @@ struct usl_ctx {
     uint32_t* topk_done;           // behind them: the count of a prediction's forward (k_count.h; 0 between calls)
     bool topk_done_clear;          // it has been cleared
     float* norm_part;         size_t norm_part_cap;  // [parts of the batch][2][d] sums of the layer norm's weight and bias gradients
+    char* gated_scratch;      size_t gated_scratch_cap;  // the gated block's backward pass: gradients by its projections, e, sums of grad_e (k_gated_grad.hip)
+    char* list_part;          size_t list_part_cap;  // losses against short lists: sums of segments, rows, rows' losses (k_list_loss.hip)
     float* gw_part;           size_t gw_part_cap;   // [groups][m*k] partial weight gradients of a split batch
     int gw_parts_most;             // groups that it has room for (0: not known yet)
     float* gxT;               size_t gxT_cap;  // [tiles][d][32] input gradient in the same layout
@@ -296,6 +298,17 @@ usl_status usl_launch_forward_mx4(usl_ctx* ctx, const void* x, const int32_t* id
 usl_status usl_launch_forward_mx4_any(usl_ctx* ctx, const void* x, const int32_t* idx, const uint32_t* codes, const uint8_t* scales, float* out, int32_t b);   // any k, any d
 usl_status usl_launch_adjust(usl_ctx* ctx, const float* out, const usl_adjustments* adj, float* adjusted, int32_t b);
 usl_status usl_launch_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustments* adj, int32_t b, int32_t kk, int32_t* top_lab, float* top_val);
+// The block in front of the layer (k_gated.hip, k_gated_grad.hip, k_int8.hip) and the losses against short lists (k_list_loss.hip).
+usl_status usl_launch_gated(usl_ctx* ctx, const void* e, const void* V_gate, const void* V_up, int32_t w, int32_t act, void* x, void* gate, void* up, int32_t b);
+usl_status usl_launch_gated_backward(usl_ctx* ctx, const float* grad_x, const void* e, const void* V_gate, const void* V_up, const void* gate, const void* up,
+                                     int32_t w, int32_t act, float* grad_e, float* grad_V_gate, float* grad_V_up, int32_t b);
+usl_status usl_launch_quantize_i8(usl_ctx* ctx, const void* rows, int64_t n, int32_t w, int8_t* codes, float* scales);
+usl_status usl_launch_dense_i8(usl_ctx* ctx, const int8_t* e, const float* e_scales, const int8_t* V0, const float* s0, const int8_t* V1 /* NULL: one matrix */,
+                               const float* s1, int32_t w, int32_t act, void* x, int32_t b);
+usl_status usl_launch_distill(usl_ctx* ctx, const float* out, const int64_t* off, const int32_t* lab, const float* logit, float temperature, float scale,
+                              float* g, float* loss, int32_t b);
+usl_status usl_launch_policy(usl_ctx* ctx, const float* out, const int64_t* off, const int32_t* lab, const float* old_logp, const float* ref_logp,
+                             const float* advantage, float clip_low, float clip_high, float beta, float scale, float* g, float* logp, float* loss, int32_t b);
 size_t usl_adjusted_segments(const usl_ctx* ctx);   // sets of candidates that usl_launch_topk_adjusted leaves at most
 static inline int usl_forward_few_blocks(const usl_ctx* c) { return c->num_cu * 2; }   // workgroups of its forward at most
 // dst_idx[q][:] = idx[rows[q]][:] and (if W) dst_W[q][:] = W[rows[q]][:], q < n; row ids are clamped into [0, m)

@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libusl.so")
 
 USL_OK, USL_EINVAL, USL_ESHAPE, USL_ENOMEM, USL_EHIP, USL_EUNSUPPORTED, USL_ESTALE = range(7)
 USL_F32, USL_BF16 = 0, 1
+USL_SILU, USL_GELU = 0, 1
 STATUS_NAMES = ["USL_OK", "USL_EINVAL", "USL_ESHAPE", "USL_ENOMEM", "USL_EHIP", "USL_EUNSUPPORTED", "USL_ESTALE"]
 
 # every symbol include/usl.h declares
@@ -23,7 +24,9 @@ SYMBOLS = ["usl_bce_loss_grad_noalloc", "usl_check", "usl_create", "usl_destroy"
            "usl_backward_weight", "usl_backward_input", "usl_backward", "usl_adam_step", "usl_redistribute",
            "usl_validate_indices", "usl_philox_words",
            "usl_layer_norm", "usl_layer_norm_backward", "usl_quantize_mx4", "usl_dequantize_mx4", "usl_forward_mx4",
-           "usl_adjust_scores", "usl_topk_adjusted"]
+           "usl_adjust_scores", "usl_topk_adjusted",
+           "usl_gated_block", "usl_gated_block_backward", "usl_quantize_i8", "usl_project_i8", "usl_gated_block_i8",
+           "usl_distill_loss_grad", "usl_policy_loss_grad"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError("libusl.so is not built: run `python -m paper_2306_03725_amd.build` "
@@ -74,6 +77,13 @@ _sig = {
     "usl_forward_mx4": [_vp, _vp, _vp, _vp, _vp, _vp, _i32],
     "usl_adjust_scores": [_vp, _vp, ctypes.POINTER(_Adjustments), _vp, _i32],
     "usl_topk_adjusted": [_vp, _vp, ctypes.POINTER(_Adjustments), _i32, _i32, _vp, _vp],
+    "usl_gated_block": [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32],
+    "usl_gated_block_backward": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32],
+    "usl_quantize_i8": [_vp, _vp, _i64, _i32, _vp, _vp],
+    "usl_project_i8": [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32],
+    "usl_gated_block_i8": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32],
+    "usl_distill_loss_grad": [_vp, _vp, _vp, _vp, _vp, _f32, _f32, _vp, _vp, _i32],
+    "usl_policy_loss_grad": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _vp, _vp, _vp, _i32],
 }
 for _name, _args in _sig.items():
     _f = getattr(_lib, _name)
@@ -104,6 +114,13 @@ def _ptr(t):
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return t.data_ptr()
+
+
+def _entries(t, off):
+    """Address of what stands for each entry of the lists that begin at off.  A tensor without elements has no address: any will do, no list has an entry."""
+    if t is None or isinstance(t, int) or t.numel():
+        return _ptr(t)
+    return _ptr(off)
 
 
 class Adjustments:
@@ -269,3 +286,31 @@ class Layer:
 
     def topk_adjusted(self, out, adjustments, b, kk, top_lab, top_val):
         self._ck(_lib.usl_topk_adjusted(self._h, _ptr(out), ctypes.byref(adjustments._a), b, kk, _ptr(top_lab), _ptr(top_val)))
+
+    def gated_block(self, e, V_gate, V_up, w, act, x, gate, up, b):
+        self._ck(_lib.usl_gated_block(self._h, _ptr(e), _ptr(V_gate), _ptr(V_up), w, act, _ptr(x), _ptr(gate), _ptr(up), b))
+
+    def gated_block_backward(self, grad_x, e, V_gate, V_up, gate, up, w, act, grad_e, grad_V_gate, grad_V_up, b):
+        self._ck(_lib.usl_gated_block_backward(self._h, _ptr(grad_x), _ptr(e), _ptr(V_gate), _ptr(V_up), _ptr(gate), _ptr(up), w, act,
+                                               _ptr(grad_e), _ptr(grad_V_gate), _ptr(grad_V_up), b))
+
+    def quantize_i8(self, rows, n, w, codes, scales):
+        self._ck(_lib.usl_quantize_i8(self._h, _ptr(rows), n, w, _ptr(codes), _ptr(scales)))
+
+    def project_i8(self, e_codes, e_scales, V_codes, V_scales, w, h, b):
+        self._ck(_lib.usl_project_i8(self._h, _ptr(e_codes), _ptr(e_scales), _ptr(V_codes), _ptr(V_scales), w, _ptr(h), b))
+
+    def gated_block_i8(self, e_codes, e_scales, gate_codes, gate_scales, up_codes, up_scales, w, act, x, b):
+        self._ck(_lib.usl_gated_block_i8(self._h, _ptr(e_codes), _ptr(e_scales), _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes),
+                                         _ptr(up_scales), w, act, _ptr(x), b))
+
+    def distill_loss_grad(self, out, tea_off, tea_lab, tea_logit, temperature, scale, g, loss, b):
+        self._ck(_lib.usl_distill_loss_grad(self._h, _ptr(out), _ptr(tea_off), _entries(tea_lab, tea_off), _entries(tea_logit, tea_off),
+                                            temperature, scale, _ptr(g), _ptr(loss), b))
+
+    def policy_loss_grad(self, out, act_off, act_lab, old_logp, ref_logp, advantage, clip_low, clip_high, beta, scale, g, logp, loss, b):
+        if logp is not None and not isinstance(logp, int) and logp.numel() == 0:
+            logp = None   # no entries, no results
+        self._ck(_lib.usl_policy_loss_grad(self._h, _ptr(out), _ptr(act_off), _entries(act_lab, act_off), _entries(old_logp, act_off),
+                                           _entries(ref_logp, act_off), _entries(advantage, act_off), clip_low, clip_high, beta, scale,
+                                           _ptr(g), _ptr(logp), _ptr(loss), b))
