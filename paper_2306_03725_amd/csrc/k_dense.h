@@ -64,22 +64,23 @@ __device__ __forceinline__ i32x4 buffer_at(const void* p) {
 __device__ __forceinline__ void to_lds(uint32_t to, const i32x4& buffer, uint32_t off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(off), "s"(buffer) : "memory");
 }
-__device__ __forceinline__ void landed() {   // what this wavefront asked for is there; behind a barrier, what all did
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+template <int LATER>   // what this wavefront asked for is there, but for the LATER loads behind it; behind a barrier, what all did
+__device__ __forceinline__ void landed() {
+    static_assert(LATER < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
 }
 
-// The n values (bytes: n * sizeof(T)) from p on, zeros behind them.  n may be 0 or less; 16 bytes at most.
-template <typename T>
-__device__ __forceinline__ i32x4 sixteen(const char* p, int bytes) {
+// The `bytes` bytes from p on, zeros behind them; may be 0 or less.  before: bytes of the same row that lie before p.  Any address.
+__device__ __forceinline__ i32x4 sixteen(const char* p, int bytes, int before) {
     if (bytes >= 16) return *reinterpret_cast<const i32x4_any*>(p);
-    i32x4 r = {0, 0, 0, 0};
-    T v[16 / sizeof(T)];
-    __builtin_memcpy(v, &r, 16);
-#pragma unroll
-    for (int j = 0; j < (int)(16 / sizeof(T)); ++j)
-        if ((j + 1) * (int)sizeof(T) <= bytes) v[j] = reinterpret_cast<const T*>(p)[j];
-    __builtin_memcpy(&r, v, 16);
-    return r;
+    unsigned __int128 r = 0;
+    if (bytes > 0 && before + bytes >= 16) {   // the last 16 bytes of the row, without those before p
+        r = __builtin_bit_cast(unsigned __int128, *reinterpret_cast<const i32x4_any*>(p - (16 - bytes))) >> 8 * (16 - bytes);
+    } else {
+#pragma unroll 1
+        for (int j = 0; j < bytes; ++j) r |= (unsigned __int128)(uint8_t)p[j] << 8 * j;
+    }
+    return __builtin_bit_cast(i32x4, r);
 }
 
 // ---- KC: ROWS rows of KB (128 or 64) bytes of K
@@ -114,13 +115,17 @@ struct StageKC {
         }
     }
     // the same through registers, for rows at any address: fetch, then (behind the step before) put
-    template <typename T>
-    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int rows, uint32_t pitch, int left) {
+    // (before: bytes of K before the step)
+    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int rows, uint32_t pitch, int left, int before) {
+        if (left >= KB) {
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) {
-            const int g = group_of(t) * 16;
-            const char* p = from + (size_t)min(row_of(t), rows - 1) * pitch + g;
-            held[t] = left >= KB ? *reinterpret_cast<const i32x4_any*>(p) : sixteen<T>(p, left - g);
+            for (int t = 0; t < LOADS; ++t) held[t] = *reinterpret_cast<const i32x4_any*>(from + (size_t)min(row_of(t), rows - 1) * pitch + group_of(t) * 16);
+        } else {
+#pragma unroll
+            for (int t = 0; t < LOADS; ++t) {
+                const int g = group_of(t) * 16;
+                held[t] = sixteen(from + (size_t)min(row_of(t), rows - 1) * pitch + g, left - g, before + g);
+            }
         }
     }
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {
@@ -157,11 +162,17 @@ struct StageKO {
             to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, k < depth && g < width ? (uint32_t)k * (uint32_t)pitch + (uint32_t)g : NOWHERE);
         }
     }
-    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int depth, size_t pitch, int width) {
+    // (before: bytes of a row before the first column)
+    static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int depth, size_t pitch, int width, int before) {
+        if (depth >= DEPTH && width >= ROW) {
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) {
-            const int g = group_of(t) * 16, k = row_of(t);
-            held[t] = sixteen<T>(from + (size_t)k * pitch + g, k < depth ? width - g : 0);
+            for (int t = 0; t < LOADS; ++t) held[t] = *reinterpret_cast<const i32x4_any*>(from + (size_t)row_of(t) * pitch + group_of(t) * 16);
+        } else {
+#pragma unroll
+            for (int t = 0; t < LOADS; ++t) {
+                const int g = group_of(t) * 16, k = row_of(t);
+                held[t] = sixteen(from + (size_t)k * pitch + g, k < depth ? width - g : 0, before + g);
+            }
         }
     }
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {
@@ -191,27 +202,59 @@ struct StageKO {
 };
 
 // ---- the block's activations
+// 1 / (1 + exp(-a)), by the hardware's exponential and reciprocal (each off by one unit in the last place; the exponent's rounding adds |a| of them to the
+// exponential, which beside 1 has no weight where |a| is large): twelve instructions less than with the library's, and the epilogue's arithmetic counts.
+__device__ __forceinline__ float sigmoid_of(float a) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.44269504f)); }
+// Phi(a), the normal distribution's function, and its density.  erfc by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (off by
+// 1.5e-7 at most, so Phi by 7.5e-8 and what the arithmetic adds: 2.3 half steps of float32 below 1): a fifth of the instructions of the library's erff.
+__device__ __forceinline__ float phi_of(float a, float& density) {
+    const float x = fabsf(a) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f)), e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
+    const float tail = 0.5f * e * t * fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    density = 0.39894228f * e;
+    return a < 0.f ? tail : 1.f - tail;
+}
 template <int ACT>   // 0: a / (1 + exp(-a)); 1: a * Phi(a), the normal distribution's function
 __device__ __forceinline__ float act_of(float a) {
-    if (ACT == 0) return a / (1.f + expf(-a));
-    return 0.5f * a * (1.f + erff(a * 0.70710678f));
+    if (ACT == 0) return a * sigmoid_of(a);
+    float density;
+    return a * phi_of(a, density);
 }
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float a, float& value, float& slope) {
     if (ACT == 0) {
-        const float p = 1.f / (1.f + expf(-a));
+        const float p = sigmoid_of(a);
         value = a * p;
-        slope = p * (1.f + a * (1.f - p));
+        slope = fmaf(value, 1.f - p, p);
     } else {
-        const float phi = 0.5f * (1.f + erff(a * 0.70710678f));
+        float density;
+        const float phi = phi_of(a, density);
         value = a * phi;
-        slope = phi + a * 0.39894228f * expf(-0.5f * a * a);
+        slope = fmaf(a, density, phi);
     }
 }
 
 template <typename T> __device__ __forceinline__ T narrow(float v);
 template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
-template <> __device__ __forceinline__ bf16 narrow<bf16>(float v) { return bf16{usl_f32_to_bf16(v)}; }
+template <> __device__ __forceinline__ bf16 narrow<bf16>(float v) { return __builtin_bit_cast(bf16, (__bf16)v); }   // nearest, ties to even
+// N neighbours (a multiple of 4) to memory at any address; `there` of them exist (1 at least)
+template <typename T, int N>
+__device__ __forceinline__ void put_many(T* to, const float (&v)[N], int there) {
+    constexpr int BYTES = N * (int)sizeof(T), WIDE = BYTES % 16 == 0 ? 4 : 2;   // words of a store
+    typedef uint32_t Words __attribute__((ext_vector_type(WIDE), aligned(2)));
+    T r[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = narrow<T>(v[j]);
+    if (there >= N) {
+        Words q[BYTES / 4 / WIDE];
+        __builtin_memcpy(q, r, BYTES);
+#pragma unroll
+        for (int u = 0; u < BYTES / 4 / WIDE; ++u) reinterpret_cast<Words*>(to)[u] = q[u];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N - 1; ++j)
+            if (j < there) to[j] = r[j];
+    }
+}
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(bf16 v) { return usl_bf16_to_f32(v.bits); }
 

@@ -14,54 +14,63 @@ struct Forward {
     int tiles_d, tiles_b;
 };
 
-// Four neighbours of an instance's output from their sums
-template <typename T, typename TO, int MATS, int ACT>
-__device__ __forceinline__ void finish(const Forward& a, const typename Core<T>::Acc (&acc)[MATS], int i, int d0, bool aligned) {
-    float v[MATS][4];
+// What 8-bit integers' sums are multiplied by: a lane's N neighbours of each matrix
+template <typename T, int MATS, int N>
+struct Scales {
+    float v[MATS][N];
+    __device__ __forceinline__ void load(const Forward& a, int d0) {
+        if (sizeof(T) == 1)
 #pragma unroll
-    for (int q = 0; q < MATS; ++q)
+            for (int q = 0; q < MATS; ++q)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[q][j] = (float)acc[q][j];
-            if (sizeof(T) == 1) v[q][j] *= a.e_scale[i] * a.V_scale[q][min(d0 + j, a.d - 1)];
-        }
-    const size_t at = (size_t)i * a.d + d0;
-    auto put = [&](void* to, const float (&f)[4]) {
-        TO r[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = narrow<TO>(f[j]);
-        TO* p = (TO*)to + at;
-        if (aligned && d0 + 3 < a.d) {
-            struct alignas(4 * sizeof(TO)) Four { TO v[4]; };
-            *reinterpret_cast<Four*>(p) = *reinterpret_cast<const Four*>(__builtin_assume_aligned(r, 4));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (d0 + j < a.d) p[j] = r[j];
-        }
-    };
-    if (MATS == 1) {
-        put(a.x, v[0]);
-        return;
+                for (int j = 0; j < N; ++j) v[q][j] = a.V_scale[q][min(d0 + j, a.d - 1)];
     }
-    float x[4];
+};
+// 16 instances' values of WD neighbouring activations, a lane N of one instance's, to rows of memory: through LDS, so that a store takes whole lines of it.
+// (16 rows of 64 bytes to a store, the other half of every line by the next one: 512 x 768 -> 32768 bfloat16, three outputs, 85 us, and with more between the
+// two 98; in whole lines 73.)  `mine`: the wavefront's own LDS.
+template <typename TO, int WD, int N>
+__device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N], int i0, int b, int d0, int d) {
+    constexpr int ROW = WD * (int)sizeof(TO), PITCH = ROW + 16, EACH = 16 / (int)sizeof(TO), GROUPS = ROW / 16;
+    static_assert(N * 4 == WD, "four lanes share a row");
+    const int l = (int)threadIdx.x & 63;
+    TO r[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
-    put(a.x, x);
-    if (a.gate) put(a.gate, v[0]);
-    if (a.up) put(a.up, v[MATS - 1]);
+    for (int j = 0; j < N; ++j) r[j] = narrow<TO>(v[j]);
+    uint4 q[N / EACH > 0 ? N / EACH : 1];
+    __builtin_memcpy(q, r, sizeof(r));
+#pragma unroll
+    for (int u = 0; u < N / EACH; ++u) *reinterpret_cast<uint4*>(mine + (l & 15) * PITCH + (l >> 4) * (ROW / 4) + u * 16) = q[u];
+#pragma unroll
+    for (int t = 0; t < 16 * GROUPS / 64; ++t) {
+        const int at = t * 64 + l, row = at / GROUPS, c = d0 + at % GROUPS * EACH, i = i0 + row;
+        const uint4 w = *reinterpret_cast<const uint4*>(mine + row * PITCH + at % GROUPS * 16);
+        if (i >= b || c >= d) continue;
+        TO* p = to + (size_t)i * d + c;
+        if (d - c >= EACH) {
+            typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
+        } else {
+            TO one[EACH];
+            __builtin_memcpy(one, &w, 16);
+#pragma unroll
+            for (int j = 0; j < EACH - 1; ++j)
+                if (j < d - c) p[j] = one[j];
+        }
+    }
 }
 
-// A tile of BD activations of BB instances.  DIRECT: rows and bases are multiples of 16 bytes.
-template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, bool DIRECT>
-__global__ void __launch_bounds__(64 * WAVES_D * WAVES_B)
+// A tile of BD activations of BB instances.  DIRECT: rows and bases are multiples of 16 bytes; STAGES steps of K then have room in LDS, one being
+// multiplied and the others on their way.  Else the tiles come through registers, two steps ahead.
+template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
+__global__ void __launch_bounds__(64 * WAVES_D * WAVES_B, 2)   // (two wavefronts to a SIMD: sums and fragments in 256 registers)
 k_dense_forward(Forward a) {
-    constexpr int WAVES = WAVES_D * WAVES_B, KB = 128, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16;
+    constexpr int WAVES = WAVES_D * WAVES_B, KB = 64, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16, AHEAD = STAGES - 1;
     using Acc = typename Core<T>::Acc;
-    using SV = StageKC<BD, KB, FD, WAVES>;
+    using SV = StageKC<BD, KB, FD, WAVES>;   // (a lane's neighbours of all fragments are neighbours)
     using SE = StageKC<BB, KB, 1, WAVES>;
-    constexpr int STEP = MATS * SV::BYTES + SE::BYTES;
-    extern __shared__ __align__(1024) char lds[];   // two steps
+    constexpr int STEP = MATS * SV::BYTES + SE::BYTES, LOADS = MATS * SV::LOADS + SE::LOADS;
+    extern __shared__ __align__(1024) char lds[];
     // Workgroups go to the chiplets in turn: the tiles of one piece of V, which share its rows, go to one of them, one after the other.
     const int turn = (int)blockIdx.x >> 3, td = turn / a.tiles_b * 8 + ((int)blockIdx.x & 7), tb = turn % a.tiles_b;
     if (td >= a.tiles_d) return;
@@ -80,63 +89,100 @@ k_dense_forward(Forward a) {
 #pragma unroll
             for (int h = 0; h < FB; ++h) acc[q][f][h] = Acc{0, 0, 0, 0};
     const int steps = (a.row_bytes + KB - 1) / KB;
-    i32x4 held_v[DIRECT ? 1 : MATS][SV::LOADS], held_e[SE::LOADS];
-    auto ask = [&](int s) {
-        const int at = s * KB, left = a.row_bytes - at;
-        char* to = lds + (s & 1) * STEP;
+    auto multiply = [&](const char* from) {
+        i32x4 eb[FB];
 #pragma unroll
-        for (int q = 0; q < MATS; ++q) {
-            if constexpr (DIRECT) SV::direct(lds_at(to + q * SV::BYTES), V[q] + at, rows_d, pitch, left);
-            else SV::template fetch<T>(held_v[q], V[q] + at, rows_d, pitch, left);
-        }
-        if constexpr (DIRECT) SE::direct(lds_at(to + MATS * SV::BYTES), e + at, rows_b, pitch, left);
-        else SE::template fetch<T>(held_e, e + at, rows_b, pitch, left);
-    };
-    auto place = [&](int s) {
-        if constexpr (!DIRECT) {
-            char* to = lds + (s & 1) * STEP;
+        for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + MATS * SV::BYTES, wb, f, 0);
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) SV::put(to + q * SV::BYTES, held_v[q]);
-            SE::put(to + MATS * SV::BYTES, held_e);
-        }
-    };
-    ask(0);
-    place(0);
-    for (int s = 0; s < steps; ++s) {
-        if (DIRECT) landed();
-        __syncthreads();   // step s is there, and nobody reads the one before it any more
-        if (s + 1 < steps) ask(s + 1);
-        const char* from = lds + (s & 1) * STEP;
-#pragma unroll
-        for (int h = 0; h < KB / 64; ++h) {
-            i32x4 eb[FB];
-#pragma unroll
-            for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + MATS * SV::BYTES, wb, f, h);
-#pragma unroll
-            for (int q = 0; q < MATS; ++q)
-#pragma unroll
-                for (int f = 0; f < FD; ++f) {
-                    const i32x4 v = SV::frag(from + q * SV::BYTES, wd, f, h);
-#pragma unroll
-                    for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
-                }
-        }
-        if (s + 1 < steps) place(s + 1);
-    }
-    const int l = (int)threadIdx.x & 63;
-    const bool aligned = a.d % 4 == 0 && ((uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.up) % (4 * sizeof(TO)) == 0;
-#pragma unroll
-    for (int g = 0; g < FB; ++g) {
-        const int i = b0 + wb + g * 16 + (l & 15);
-        if (i < a.b)
+        for (int q = 0; q < MATS; ++q)
 #pragma unroll
             for (int f = 0; f < FD; ++f) {
-                const int at = d0 + wd + frag_row<FD>(f, (l >> 4) * 4);
-                Acc one[MATS];
+                const i32x4 v = SV::frag(from + q * SV::BYTES, wd, f, 0);
 #pragma unroll
-                for (int q = 0; q < MATS; ++q) one[q] = acc[q][f][g];
-                if (at < a.d) finish<T, TO, MATS, ACT>(a, one, i, at, aligned);
+                for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
             }
+    };
+    if constexpr (DIRECT) {
+        auto ask = [&](int s, int place) {
+            const int at = s * KB, left = a.row_bytes - at;
+            const uint32_t to = lds_at(lds + place * STEP);
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) SV::direct(to + q * SV::BYTES, V[q] + at, rows_d, pitch, left);
+            SE::direct(to + MATS * SV::BYTES, e + at, rows_b, pitch, left);
+        };
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+            if (s < steps) ask(s, s);
+        int here = 0, next = AHEAD;   // step s's place, and that of step s + AHEAD (where step s - 1 was)
+        for (int s = 0; s < steps; ++s) {
+            if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();   // step s, but for the steps behind it
+            else landed<0>();
+            __syncthreads();   // for all wavefronts, and nobody reads step s - 1 any more
+            if (s + AHEAD < steps) ask(s + AHEAD, next);
+            multiply(lds + here * STEP);
+            here = here + 1 == STAGES ? 0 : here + 1;
+            next = next + 1 == STAGES ? 0 : next + 1;
+        }
+    } else {
+        struct Held { i32x4 v[MATS][SV::LOADS], e[SE::LOADS]; };
+        Held one, two;   // steps s + 1 and s + 2
+        auto ask = [&](Held& h, int s) {
+            if (s >= steps) return;
+            const int at = s * KB, left = a.row_bytes - at;
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) SV::fetch(h.v[q], V[q] + at, rows_d, pitch, left, at);
+            SE::fetch(h.e, e + at, rows_b, pitch, left, at);
+        };
+        auto place = [&](const Held& h, int s) {
+            if (s >= steps) return;
+            char* to = lds + (s & 1) * STEP;
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) SV::put(to + q * SV::BYTES, h.v[q]);
+            SE::put(to + MATS * SV::BYTES, h.e);
+        };
+        ask(two, 0);
+        ask(one, 1);
+        place(two, 0);
+        for (int s = 0; s < steps; s += 2) {
+            __syncthreads();
+            ask(two, s + 2);
+            multiply(lds);
+            place(one, s + 1);
+            __syncthreads();
+            if (s + 1 >= steps) break;
+            ask(one, s + 3);
+            multiply(lds + STEP);
+            place(two, s + 2);
+        }
+    }
+    constexpr int N = 4 * FD, WD = BD / WAVES_D;
+    static_assert(WAVES * 16 * (WD * (int)sizeof(TO) + 16) <= (DIRECT ? STAGES : 2) * STEP, "room for the outputs");
+    const int l = (int)threadIdx.x & 63, i0 = b0 + wb, c0 = d0 + wd;
+    char* mine = lds + wave * 16 * (WD * (int)sizeof(TO) + 16);
+    Scales<T, MATS, N> scales;
+    scales.load(a, c0 + (l >> 4) * N);
+    __syncthreads();   // the last step has been read
+#pragma unroll
+    for (int g = 0; g < FB; ++g) {
+        const float e_scale = sizeof(T) == 1 ? a.e_scale[min(i0 + g * 16 + (l & 15), a.b - 1)] : 1.f;
+        float v[MATS][N];
+#pragma unroll
+        for (int q = 0; q < MATS; ++q)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                v[q][j] = (float)acc[q][j / 4][g][j % 4];
+                if (sizeof(T) == 1) v[q][j] *= e_scale * scales.v[q][j];
+            }
+        if (MATS == 1) {
+            put_tile<TO, WD, N>(mine, (TO*)a.x, v[0], i0 + g * 16, a.b, c0, a.d);
+            continue;
+        }
+        float x[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
+        put_tile<TO, WD, N>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d);
+        if (a.gate) put_tile<TO, WD, N>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d);
+        if (a.up) put_tile<TO, WD, N>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d);
     }
 }
 
@@ -164,10 +210,10 @@ k_dense_few(Forward a) {
         for (int q = 0; q < MATS; ++q) acc[q] = Core<T>::mul(*reinterpret_cast<const i32x4_any*>(V[q] + (size_t)s * 64), y, acc[q]);
     }
     if (whole < steps && first <= whole && whole < first + each) {   // the end of the rows
-        const int left = a.row_bytes - whole * 64 - (l >> 4) * 16;
-        const i32x4 y = sixteen<T>(e + (size_t)whole * 64, left);
+        const int before = whole * 64 + (l >> 4) * 16, left = a.row_bytes - before;
+        const i32x4 y = sixteen(e + (size_t)whole * 64, left, before);
 #pragma unroll
-        for (int q = 0; q < MATS; ++q) acc[q] = Core<T>::mul(sixteen<T>(V[q] + (size_t)whole * 64, left), y, acc[q]);
+        for (int q = 0; q < MATS; ++q) acc[q] = Core<T>::mul(sixteen(V[q] + (size_t)whole * 64, left, before), y, acc[q]);
     }
 #pragma unroll
     for (int q = 0; q < MATS; ++q) sums[wave][q][l] = acc[q];
@@ -177,19 +223,40 @@ k_dense_few(Forward a) {
     for (int q = 0; q < MATS; ++q)
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) acc[q] += sums[v][q][l];
-    const bool aligned = a.d % 4 == 0 && ((uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.up) % (4 * sizeof(TO)) == 0;
     const int at = d0 + (l >> 4) * 4;
-    if ((l & 15) < a.b && at < a.d) finish<T, TO, MATS, ACT>(a, acc, l & 15, at, aligned);
+    if ((l & 15) < a.b && at < a.d) {
+        Scales<T, MATS, 4> scales;
+        scales.load(a, at);
+        const float e_scale = sizeof(T) == 1 ? a.e_scale[l & 15] : 1.f;
+        float v[MATS][4];
+#pragma unroll
+        for (int q = 0; q < MATS; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[q][j] = (float)acc[q][j];
+                if (sizeof(T) == 1) v[q][j] *= e_scale * scales.v[q][j];
+            }
+        const size_t to = (size_t)(l & 15) * a.d + at;
+        if (MATS == 1) {
+            put_many((TO*)a.x + to, v[0], a.d - at);
+            return;
+        }
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
+        put_many((TO*)a.x + to, x, a.d - at);
+        if (a.gate) put_many((TO*)a.gate + to, v[0], a.d - at);
+        if (a.up) put_many((TO*)a.up + to, v[MATS - 1], a.d - at);
+    }
 }
 
-template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B>
+template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
 usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
-    constexpr int BYTES = 2 * (MATS * BD + BB) * 128;
+    constexpr int BYTES = (DIRECT ? STAGES : 2) * (MATS * BD + BB) * 64;
+    const auto kernel = k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, STAGES, DIRECT>;
     a.tiles_d = (a.d + BD - 1) / BD;
     a.tiles_b = (a.b + BB - 1) / BB;
     const dim3 grid((unsigned)((a.tiles_d + 7) / 8 * 8 * a.tiles_b)), block(64 * WAVES_D * WAVES_B);
-    const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
-    const auto kernel = direct ? k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, true> : k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, false>;
     if (BYTES > 64 * 1024) USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     hipLaunchKernelGGL(kernel, grid, block, BYTES, c->stream, a);
     return usl_check_launch(c, what);
@@ -201,8 +268,16 @@ usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
         hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
-    if ((int64_t)((a.d + 127) / 128) * ((a.b + 127) / 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2>(c, a, what);
-    return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2>(c, a, what);
+    constexpr int BD = MATS == 1 ? 256 : 128;
+    const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
+    auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
+    if (direct) {
+        if (a.b > 128 && tiles(BD, 256) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, BD, 256, 2, 4, 4, true>(c, a, what);
+        if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what);
+        return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what);
+    }
+    if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
+    return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
 }
 
 }  // namespace dense

@@ -12,7 +12,6 @@ using namespace dense;
 
 namespace {
 
-constexpr int PAD = 128;   // columns of G and of e's copy are padded to it
 constexpr int PREP_NT = 256;
 
 template <typename T> constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
@@ -26,6 +25,7 @@ struct Grad {
     int d, w, dp, wp, b;       // b: instances of this chunk
     int rows;                  // padded instances of the chunk
     int first;                 // not 0: grad_V is overwritten, else added to
+    int tiles_m, tiles_n;      // of a product
     int splits, steps_each;    // of grad_e's sums over d
 };
 
@@ -46,81 +46,145 @@ template <> __device__ __forceinline__ void split<bf16>(float v, bf16 (&part)[3]
     part[2] = bf16{(uint16_t)(__float_as_uint(last) >> 16)};
 }
 
-// G and e's copy.  Grid: (columns of G / PREP_NT + columns of e / PREP_NT, rows)
+// G and e's copy, eight columns a lane.  Grid: (groups of 8 columns of G and of e / PREP_NT, rows).  Bound by its bytes.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(PREP_NT)
 k_gated_slopes(Grad a) {
-    const int i = (int)blockIdx.y, blocks = (a.dp + PREP_NT - 1) / PREP_NT;
-    if ((int)blockIdx.x >= blocks) {
-        const int c = ((int)blockIdx.x - blocks) * PREP_NT + (int)threadIdx.x;
-        if (c < a.wp) ((T*)a.E)[(size_t)i * a.wp + c] = i < a.b && c < a.w ? ((const T*)a.e)[(size_t)i * a.w + c] : narrow<T>(0.f);
+    constexpr int N = 8;
+    struct Eight { T v[N]; };
+    typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+    auto load = [](const auto* p, auto& v) {   // from any address
+        Any q[sizeof(v) / 16];
+#pragma unroll
+        for (int u = 0; u < (int)(sizeof(v) / 16); ++u) q[u] = reinterpret_cast<const Any*>(p)[u];
+        __builtin_memcpy(&v, q, sizeof(v));
+    };
+    auto store = [](T* p, const Eight& v) {
+        uint4 q[sizeof(v) / 16];
+        __builtin_memcpy(q, &v, sizeof(v));
+#pragma unroll
+        for (int u = 0; u < (int)(sizeof(v) / 16); ++u) reinterpret_cast<uint4*>(p)[u] = q[u];
+    };
+    const int i = (int)blockIdx.y, groups = a.dp / N;
+    int c = ((int)blockIdx.x * PREP_NT + (int)threadIdx.x);
+    if (c >= groups) {
+        c = (c - groups) * N;
+        if (c >= a.wp) return;
+        Eight v;
+        const T* e = (const T*)a.e + (size_t)i * a.w + c;
+        if (i < a.b && c + N <= a.w) load(e, v.v);
+        else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) v.v[j] = i < a.b && c + j < a.w ? e[j] : narrow<T>(0.f);
+        }
+        store((T*)a.E + (size_t)i * a.wp + c, v);
         return;
     }
-    const int c = (int)blockIdx.x * PREP_NT + (int)threadIdx.x;
-    if (c >= a.dp) return;
-    float by_gate = 0.f, by_up = 0.f;
-    if (i < a.b && c < a.d) {
+    c *= N;
+    float by_gate[N], by_up[N];
+    {
+        T gate[N], up[N];
+        float g[N];
         const size_t at = (size_t)i * a.d + c;
-        float value, slope;
-        act_and_slope<ACT>(widen(((const T*)a.gate)[at]), value, slope);
-        const float g = a.grad_x[at];
-        by_gate = g * widen(((const T*)a.up)[at]) * slope;
-        by_up = g * value;
+        if (i < a.b && c + N <= a.d) {
+            load((const T*)a.gate + at, gate);
+            load((const T*)a.up + at, up);
+            load(a.grad_x + at, g);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const bool is = i < a.b && c + j < a.d;
+                gate[j] = is ? ((const T*)a.gate)[at + j] : narrow<T>(0.f);
+                up[j] = is ? ((const T*)a.up)[at + j] : narrow<T>(0.f);
+                g[j] = is ? a.grad_x[at + j] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float value, slope;
+            act_and_slope<ACT>(widen(gate[j]), value, slope);
+            by_gate[j] = g[j] * widen(up[j]) * slope;
+            by_up[j] = g[j] * value;
+        }
     }
-    T part[PARTS<T>];
     T* to = (T*)a.G + (size_t)i * 2 * a.dp + c;
     const size_t next = (size_t)a.rows * 2 * a.dp;
-    split<T>(by_gate, part);
 #pragma unroll
-    for (int q = 0; q < PARTS<T>; ++q) to[q * next] = part[q];
-    split<T>(by_up, part);
+    for (int side = 0; side < 2; ++side) {
+        Eight v[PARTS<T>];
 #pragma unroll
-    for (int q = 0; q < PARTS<T>; ++q) to[q * next + a.dp] = part[q];
+        for (int j = 0; j < N; ++j) {
+            T part[PARTS<T>];
+            split<T>(side ? by_up[j] : by_gate[j], part);
+#pragma unroll
+            for (int q = 0; q < PARTS<T>; ++q) v[q].v[j] = part[q];
+        }
+#pragma unroll
+        for (int q = 0; q < PARTS<T>; ++q) store(to + q * next + side * a.dp, v[q]);
+    }
 }
 
-// grad_V: [w] along m, [2][d] along n, the instances along K.  Tiles of 128 x 128, four wavefronts.
-template <typename T>
-__global__ void __launch_bounds__(256)
+// One of so many tiles: workgroups go to the chiplets in turn, and the `inner` tiles of an outer one, which share what they read, go to one chiplet together.
+__device__ __forceinline__ void tile_of(int inner, int& in, int& out) {
+    const int turn = (int)blockIdx.x >> 3;
+    in = turn % inner;
+    out = turn / inner * 8 + ((int)blockIdx.x & 7);
+}
+unsigned tiles_grid(int inner, int outer) { return (unsigned)((outer + 7) / 8 * 8 * inner); }
+
+// grad_V: [w] along m, [2][d] along n, the instances along K.  Tiles of MT x 128, a wavefront 64 x 64 of it.  The parts of G meet the same fragments of e, so
+// what has to come from the caches for a product on the matrix cores falls with MT.
+template <typename T, int MT, int STAGES>
+__global__ void __launch_bounds__(2 * MT, 2)
 k_gated_grad_v(Grad a) {
-    constexpr int P = PARTS<T>, F = 4;
-    using S = StageKO<T, 128, 4>;
-    constexpr int STEP = (1 + P) * S::BYTES;
-    __shared__ __align__(1024) char lds[2 * STEP];
-    const int m0 = (int)blockIdx.x * 128, n0 = (int)blockIdx.y * 128, wave = (int)threadIdx.x >> 6, wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-    const size_t pitch_e = (size_t)a.wp * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next = a.rows * pitch_g;
+    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 32, AHEAD = STAGES - 1;
+    using SE = StageKO<T, MT, WAVES>;
+    using SG = StageKO<T, 128, WAVES>;
+    constexpr int STEP = SE::BYTES + P * SG::BYTES, LOADS = SE::LOADS + P * SG::LOADS;
+    extern __shared__ __align__(1024) char lds[];
+    int tm, tn;
+    tile_of(a.tiles_m, tm, tn);
+    if (tn >= 2 * a.dp / 128) return;
+    const int m0 = tm * MT, n0 = tn * 128, wave = (int)threadIdx.x >> 6, wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    const size_t pitch_e = (size_t)a.wp * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next_part = a.rows * pitch_g;
     const char *E = a.E + (size_t)m0 * sizeof(T), *G = a.G + (size_t)n0 * sizeof(T);
     f32x4 acc[F][F];
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int h = 0; h < F; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
-    const int steps = a.rows / S::DEPTH;
-    auto ask = [&](int s) {
-        const uint32_t to = lds_at(lds + (s & 1) * STEP);
-        S::direct(to, E + (size_t)s * S::DEPTH * pitch_e, S::DEPTH, pitch_e, S::ROW);
+    const int steps = a.rows / SE::DEPTH;
+    auto ask = [&](int s, int place) {
+        const uint32_t to = lds_at(lds + place * STEP);
+        SE::direct(to, E + (size_t)s * SE::DEPTH * pitch_e, SE::DEPTH, pitch_e, SE::ROW);
 #pragma unroll
-        for (int q = 0; q < P; ++q) S::direct(to + (1 + q) * S::BYTES, G + q * next + (size_t)s * S::DEPTH * pitch_g, S::DEPTH, pitch_g, S::ROW);
+        for (int q = 0; q < P; ++q) SG::direct(to + SE::BYTES + q * SG::BYTES, G + q * next_part + (size_t)s * SE::DEPTH * pitch_g, SE::DEPTH, pitch_g, SG::ROW);
     };
-    ask(0);
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (s < steps) ask(s, s);
+    int here = 0, next = AHEAD;
     for (int s = 0; s < steps; ++s) {
-        landed();
-        __syncthreads();
-        if (s + 1 < steps) ask(s + 1);
-        const char* from = lds + (s & 1) * STEP;
+        if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();
+        else landed<0>();
+        __syncthreads();   // step s is there, and nobody reads step s - 1 any more
+        if (s + AHEAD < steps) ask(s + AHEAD, next);
+        const char* from = lds + here * STEP;
         i32x4 x[F];
 #pragma unroll
-        for (int f = 0; f < F; ++f) x[f] = S::frag(from, wm + f * 16);
+        for (int f = 0; f < F; ++f) x[f] = SE::frag(from, wm + f * 16);
 #pragma unroll
         for (int q = P - 1; q >= 0; --q)   // the small parts first
 #pragma unroll
             for (int h = 0; h < F; ++h) {
-                const i32x4 y = S::frag(from + (1 + q) * S::BYTES, wn + h * 16);
+                const i32x4 y = SG::frag(from + SE::BYTES + q * SG::BYTES, wn + h * 16);
 #pragma unroll
                 for (int f = 0; f < F; ++f) acc[f][h] = Core<T>::mul(x[f], y, acc[f][h]);
             }
+        here = here + 1 == STAGES ? 0 : here + 1;
+        next = next + 1 == STAGES ? 0 : next + 1;
     }
     const int l = (int)threadIdx.x & 63;
-    const bool aligned = a.w % 4 == 0 && ((uintptr_t)a.grad_V[0] | (uintptr_t)a.grad_V[1]) % 16 == 0;
 #pragma unroll
     for (int h = 0; h < F; ++h) {
         const int n = n0 + wn + h * 16 + (l & 15), which = n >= a.dp, row = n - which * a.dp;
@@ -130,61 +194,55 @@ k_gated_grad_v(Grad a) {
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const int m = m0 + wm + f * 16 + (l >> 4) * 4;
-            f32x4 v = acc[f][h];
-            if (aligned && m + 3 < a.w) {
-                f32x4* p = reinterpret_cast<f32x4*>(to + m);
-                if (!a.first) v += *p;
-                *p = v;
-            } else {
+            if (m >= a.w) continue;
+            float v[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (m + j < a.w) to[m + j] = a.first ? v[j] : to[m + j] + v[j];
-            }
+            for (int j = 0; j < 4; ++j) v[j] = a.first ? acc[f][h][j] : acc[f][h][j] + to[min(m + j, a.w - 1)];
+            put_many(to + m, v, a.w - m);
         }
     }
 }
 
-// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  DIRECT: V's rows and bases are multiples of 16 bytes.
-template <typename T, bool DIRECT>
-__global__ void __launch_bounds__(256)
+// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  Tiles of MT x NT, a wavefront 64 x 64 of it.  DIRECT: V's rows and bases are
+// multiples of 16 bytes; else V comes through registers, asked for two steps ahead and put into LDS one step ahead.
+template <typename T, int MT, int NT, int STAGES, bool DIRECT>
+__global__ void __launch_bounds__(MT * NT / 64, 2)
 k_gated_grad_e(Grad a) {
-    constexpr int P = PARTS<T>, F = 4;
-    using SV = StageKO<T, 128, 4>;
-    using SG = StageKC<128, 64, 1, 4>;
-    constexpr int STEP = SV::BYTES + P * SG::BYTES;
-    __shared__ __align__(1024) char lds[2 * STEP];
-    const int m0 = (int)blockIdx.x * 128, n0 = (int)blockIdx.y * 128, wave = (int)threadIdx.x >> 6, wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-    const size_t pitch_v = (size_t)a.w * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next = a.rows * pitch_g;
-    const int rows = a.rows - n0;   // (of the tile's 128; those behind the last instance hold zeros)
+    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / 64), AHEAD = STAGES - 1;
+    static_assert(DIRECT || STAGES == 3, "two steps ahead through registers");
+    using SV = StageKO<T, MT, WAVES>;
+    using SG = StageKC<NT, 64, 1, WAVES>;
+    constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (DIRECT ? SV::LOADS : 0) + P * SG::LOADS;   // (loads into registers only make a wait longer)
+    extern __shared__ __align__(1024) char lds[];
+    int tile, piece;
+    tile_of(a.tiles_m * a.tiles_n, tile, piece);
+    if (piece >= a.splits) return;
+    const int m0 = tile % a.tiles_m * MT, n0 = tile / a.tiles_m * NT, wave = (int)threadIdx.x >> 6, wm = wave % (MT / 64) * 64, wn = wave / (MT / 64) * 64;
+    const size_t pitch_v = (size_t)a.w * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next_part = a.rows * pitch_g;
+    const int rows = a.rows - n0;   // (those behind the last instance hold zeros)
     f32x4 acc[F][F];
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int h = 0; h < F; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
-    const int first = (int)blockIdx.z * a.steps_each, last = min(first + a.steps_each, 2 * a.dp / SV::DEPTH);
-    i32x4 held[SV::LOADS];
-    auto ask = [&](int s) {
-        char* to = lds + (s & 1) * STEP;
-        const int k = s * SV::DEPTH, which = k >= a.dp, row = k - which * a.dp;   // rows behind V's end meet zeros of G, and are not read
-        const char* V = (const char*)a.V[which] + (size_t)min(row, a.d - 1) * pitch_v + (size_t)m0 * sizeof(T);
-        if constexpr (DIRECT) SV::direct(lds_at(to), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
-        else SV::fetch(held, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
+    const int first = piece * a.steps_each, steps = min(a.steps_each, 2 * a.dp / SV::DEPTH - first);
+    struct Held { i32x4 v[SV::LOADS]; };
+    Held one, two;
+    auto ask = [&](int s, int place) {
+        const int k = (first + s) * SV::DEPTH;
+        const uint32_t to = lds_at(lds + place * STEP);
 #pragma unroll
         for (int q = 0; q < P; ++q)
-            SG::direct(lds_at(to + SV::BYTES + q * SG::BYTES), a.G + q * next + (size_t)n0 * pitch_g + (size_t)k * sizeof(T), rows, (uint32_t)pitch_g, 64);
+            SG::direct(to + SV::BYTES + q * SG::BYTES, a.G + q * next_part + (size_t)n0 * pitch_g + (size_t)k * sizeof(T), rows, (uint32_t)pitch_g, 64);
     };
-    auto place = [&](int s) {
-        if constexpr (!DIRECT) SV::put(lds + (s & 1) * STEP, held);
+    auto matrix = [&](int s, int place, Held& h) {
+        if (s >= steps) return;
+        const int k = (first + s) * SV::DEPTH, which = k >= a.dp, row = k - which * a.dp;   // rows behind V's end meet zeros of G, and are not read
+        const char* V = (const char*)a.V[which] + (size_t)min(row, a.d - 1) * pitch_v + (size_t)m0 * sizeof(T);
+        if constexpr (DIRECT) SV::direct(lds_at(lds + place * STEP), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
+        else SV::fetch(h.v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
     };
-    if (first < last) {
-        ask(first);
-        place(first);
-    }
-    for (int s = first; s < last; ++s) {
-        landed();
-        __syncthreads();
-        if (s + 1 < last) ask(s + 1);
-        const char* from = lds + (s & 1) * STEP;
+    auto multiply = [&](const char* from) {
         i32x4 x[F];
 #pragma unroll
         for (int f = 0; f < F; ++f) x[f] = SV::frag(from, wm + f * 16);
@@ -196,10 +254,36 @@ k_gated_grad_e(Grad a) {
 #pragma unroll
                 for (int f = 0; f < F; ++f) acc[f][h] = Core<T>::mul(x[f], y, acc[f][h]);
             }
-        if (s + 1 < last) place(s + 1);
+    };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (s < steps) {
+            ask(s, s);
+            if (DIRECT) matrix(s, s, one);
+        }
+    int here = 0, next = AHEAD;
+    auto turn = [&](int s, Held& after, Held& behind) {   // after: V of step s + 1; behind: to hold that of step s + 2
+        if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();
+        else landed<0>();
+        __syncthreads();
+        if (s + AHEAD < steps) ask(s + AHEAD, next);
+        matrix(s + AHEAD, next, behind);
+        multiply(lds + here * STEP);
+        here = here + 1 == STAGES ? 0 : here + 1;
+        next = next + 1 == STAGES ? 0 : next + 1;
+        if (!DIRECT && s + 1 < steps) SV::put(lds + here * STEP, after.v);
+    };
+    if constexpr (!DIRECT) {
+        matrix(0, 0, two);
+        matrix(1, 1, one);
+        SV::put(lds, two.v);
+    }
+    for (int s = 0; s < steps; s += 2) {
+        turn(s, one, two);
+        if (s + 1 < steps) turn(s + 1, two, one);
     }
     const int l = (int)threadIdx.x & 63;
-    float* sums = a.sums + (size_t)blockIdx.z * a.b * a.w;
+    float* sums = a.sums + (size_t)piece * a.b * a.w;
 #pragma unroll
     for (int h = 0; h < F; ++h) {
         const int i = n0 + wn + h * 16 + (l & 15);
@@ -207,56 +291,90 @@ k_gated_grad_e(Grad a) {
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const int m = m0 + wm + f * 16 + (l >> 4) * 4;
-            float* to = sums + (size_t)i * a.w + m;
-            if (a.w % 4 == 0 && m + 3 < a.w) *reinterpret_cast<f32x4*>(to) = acc[f][h];
-            else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (m + j < a.w) to[j] = acc[f][h][j];
-            }
+            if (m >= a.w) continue;
+            const float v[4] = {acc[f][h][0], acc[f][h][1], acc[f][h][2], acc[f][h][3]};
+            put_many(sums + (size_t)i * a.w + m, v, a.w - m);
         }
     }
 }
 
-// grad_e: the pieces' sums, in a fixed order
+// grad_e: the pieces' sums, in a fixed order: each of four wavefronts every fourth piece, then theirs
 __global__ void __launch_bounds__(256)
 k_gated_join(const float* __restrict__ sums, float* __restrict__ grad_e, size_t n, int splits) {
-    for (size_t v = (size_t)blockIdx.x * 256 + threadIdx.x; v < n; v += (size_t)gridDim.x * 256) {
-        float s = sums[v];
-        for (int q = 1; q < splits; ++q) s += sums[(size_t)q * n + v];
-        grad_e[v] = s;
-    }
+    __shared__ float part[4][64];
+    const int l = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const size_t v = (size_t)blockIdx.x * 64 + l, at = v < n ? v : n - 1;
+    float s = 0.f;
+#pragma unroll 8
+    for (int q = wave; q < splits; q += 4) s += sums[(size_t)q * n + at];
+    part[wave][l] = s;
+    __syncthreads();
+    if (wave == 0 && v < n) grad_e[v] = part[0][l] + part[1][l] + part[2][l] + part[3][l];
 }
 
 constexpr size_t SCRATCH = (size_t)1 << 30;   // what the chunk of instances is cut to, if 256 of them take less
+
+template <typename F>
+usl_status lds_for(usl_ctx* c, F* kernel, int bytes) {
+    if (bytes > 64 * 1024) USL_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return USL_OK;
+}
+
+template <typename T, int MT, int STAGES>
+usl_status grad_v(usl_ctx* c, Grad a) {
+    constexpr int BYTES = STAGES * (MT + PARTS<T> * 128) * 64;
+    USL_TRY(lds_for(c, k_gated_grad_v<T, MT, STAGES>, BYTES));
+    a.tiles_m = (a.w + MT - 1) / MT;
+    hipLaunchKernelGGL((k_gated_grad_v<T, MT, STAGES>), dim3(tiles_grid(a.tiles_m, 2 * a.dp / 128)), dim3(2 * MT), BYTES, c->stream, a);
+    return usl_check_launch(c, "gated_block_backward");
+}
+
+template <typename T, int MT, int NT, int STAGES, bool DIRECT>
+usl_status grad_e(usl_ctx* c, Grad a) {
+    constexpr int BYTES = STAGES * (MT + PARTS<T> * NT) * 64;
+    USL_TRY(lds_for(c, k_gated_grad_e<T, MT, NT, STAGES, DIRECT>, BYTES));
+    hipLaunchKernelGGL((k_gated_grad_e<T, MT, NT, STAGES, DIRECT>), dim3(tiles_grid(a.tiles_m * a.tiles_n, a.splits)), dim3(MT * NT / 64), BYTES, c->stream, a);
+    return usl_check_launch(c, "gated_block_backward");
+}
+
+// Tiles of grad_e: 128 columns where w has no more, instances 64 at a time where there are no more
+struct Tiles { int m, n; };
+Tiles tiles_of(int w, int rows) { return w <= 128 ? Tiles{128, 128} : rows <= 64 ? Tiles{256, 64} : Tiles{256, 128}; }
 
 template <typename T>
 usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
     constexpr int ES = (int)sizeof(T), DEPTH = 64 / ES;
     const char* what = "gated_block_backward";
-    a.dp = (a.d + PAD - 1) / PAD * PAD;
-    a.wp = (a.w + PAD - 1) / PAD * PAD;
+    a.dp = (a.d + 127) / 128 * 128;
+    a.wp = a.w <= 128 ? 128 : (a.w + 255) / 256 * 256;
     const size_t row = ((size_t)PARTS<T> * 2 * a.dp + a.wp) * ES;
     auto padded = [](size_t n) { return (n + 31) / 32 * 32; };   // a step of K, and more than a wavefront's rows
     size_t most = padded((size_t)c->max_b);
     if (most * row > SCRATCH) most = padded(SCRATCH / row < 256 ? 256 : SCRATCH / row);
     if (most > padded((size_t)c->max_b)) most = padded((size_t)c->max_b);
     if (most > 32768) most = 32768;   // a row is a grid dimension
-    const int tiles_w = a.wp / 128, k_steps = 2 * a.dp / DEPTH;
-    auto splits_of = [&](int rows) {   // two workgroups to a compute unit; at least eight steps each
-        const int tiles = tiles_w * ((rows + 127) / 128), want = (2 * c->num_cu + tiles - 1) / tiles, room = (k_steps + 7) / 8;
-        return want < room ? want : room;
+    const int k_steps = 2 * a.dp / DEPTH;
+    auto cut = [&](Grad& g, int rows) {   // a workgroup to a compute unit; at least four steps each
+        const Tiles t = tiles_of(g.w, rows);
+        g.tiles_m = (g.w + t.m - 1) / t.m;
+        g.tiles_n = (rows + t.n - 1) / t.n;
+        const int tiles = g.tiles_m * g.tiles_n, want = c->num_cu / tiles, room = (k_steps + 3) / 4;   // (one more than there is room for takes another round)
+        g.splits = want < 1 ? 1 : want < room ? want : room;
+        g.steps_each = (k_steps + g.splits - 1) / g.splits;
+        g.splits = (k_steps + g.steps_each - 1) / g.steps_each;
+        return t;
     };
     size_t sums_most = 0;
     for (size_t r = 32; r <= most; r += 32) {   // (not always the largest batch's)
-        const size_t s = (size_t)splits_of((int)r) * r * a.w;
+        Grad g = a;
+        cut(g, (int)r);
+        const size_t s = (size_t)g.splits * r * a.w;
         if (s > sums_most) sums_most = s;
     }
     USL_TRY(usl_reserve(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, most * row + sums_most * 4));
     a.G = c->gated_scratch;
     const char *e = (const char*)a.e, *gate = (const char*)a.gate, *up = (const char*)a.up;
     const float* grad_x = a.grad_x;
-    float* grad_e = a.grad_e;
     for (int32_t i0 = 0; i0 < b; i0 += (int32_t)most) {
         a.b = (int)(b - i0 < (int32_t)most ? b - i0 : (int32_t)most);
         a.rows = (int)padded((size_t)a.b);
@@ -267,26 +385,22 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         a.gate = gate + (size_t)i0 * a.d * ES;
         a.up = up + (size_t)i0 * a.d * ES;
         a.grad_x = grad_x + (size_t)i0 * a.d;
-        const dim3 slopes((unsigned)((a.dp + PREP_NT - 1) / PREP_NT + (a.wp + PREP_NT - 1) / PREP_NT), (unsigned)a.rows);
+        const dim3 slopes((unsigned)(((a.dp + a.wp) / 8 + PREP_NT - 1) / PREP_NT), (unsigned)a.rows);
         if (act == USL_SILU) hipLaunchKernelGGL((k_gated_slopes<T, 0>), slopes, dim3(PREP_NT), 0, c->stream, a);
         else hipLaunchKernelGGL((k_gated_slopes<T, 1>), slopes, dim3(PREP_NT), 0, c->stream, a);
         USL_TRY(usl_check_launch(c, what));
         if (a.grad_V[0] || a.grad_V[1]) {
-            hipLaunchKernelGGL(k_gated_grad_v<T>, dim3((unsigned)tiles_w, (unsigned)(2 * a.dp / 128)), dim3(256), 0, c->stream, a);
-            USL_TRY(usl_check_launch(c, what));
+            if (a.w <= 128) USL_TRY((grad_v<T, 128, 4>(c, a)));
+            else USL_TRY((grad_v<T, 256, 3>(c, a)));
         }
-        if (!grad_e) continue;
-        a.splits = splits_of(a.rows);
-        a.steps_each = (k_steps + a.splits - 1) / a.splits;
-        a.splits = (k_steps + a.steps_each - 1) / a.steps_each;
-        const dim3 grid((unsigned)tiles_w, (unsigned)((a.rows + 127) / 128), (unsigned)a.splits);
+        if (!a.grad_e) continue;
+        const Tiles t = cut(a, a.rows);
         const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
-        if (direct) hipLaunchKernelGGL((k_gated_grad_e<T, true>), grid, dim3(256), 0, c->stream, a);
-        else hipLaunchKernelGGL((k_gated_grad_e<T, false>), grid, dim3(256), 0, c->stream, a);
-        USL_TRY(usl_check_launch(c, what));
+        if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, true>(c, a) : grad_e<T, 128, 128, 3, false>(c, a)));
+        else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, true>(c, a) : grad_e<T, 256, 64, 3, false>(c, a)));
+        else USL_TRY((direct ? grad_e<T, 256, 128, 3, true>(c, a) : grad_e<T, 256, 128, 3, false>(c, a)));
         const size_t n = (size_t)a.b * a.w;
-        const unsigned blocks = (unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096);
-        hipLaunchKernelGGL(k_gated_join, dim3(blocks), dim3(256), 0, c->stream, a.sums, grad_e + (size_t)i0 * a.w, n, a.splits);
+        hipLaunchKernelGGL(k_gated_join, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, c->stream, a.sums, a.grad_e + (size_t)i0 * a.w, n, a.splits);
         USL_TRY(usl_check_launch(c, what));
     }
     return USL_OK;
