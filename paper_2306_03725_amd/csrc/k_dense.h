@@ -132,11 +132,17 @@ struct StageKC {
 #pragma unroll
         for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + (t * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16) = held[t];
     }
-    // fragment f's 16 bytes of this lane, 64-byte part h of the step; row0: the wavefront's first row of the tile
-    static __device__ __forceinline__ i32x4 frag(const char* lds, int row0, int f, int h) {
-        const int l = (int)(threadIdx.x & 63), row = row0 + frag_row<SPREAD>(f, l & 15);
-        return *reinterpret_cast<const i32x4*>(lds + row * KB + place_of<KB, SPREAD>(row, h * 4 + (l >> 4)) * 16);
+    // Where this lane's 16 bytes of fragment 0 lie, row0 being the wavefront's first row of the tile (a multiple of 16 * SPREAD), and how far on those of
+    // fragment f: the key of a row is that of its fragment's row.  KB = 64.
+    static __device__ __forceinline__ int lane(int row0) {
+        static_assert(KB == 64, "a fragment is a step");
+        const int l = (int)threadIdx.x & 63, row = row0 + frag_row<SPREAD>(0, l & 15);
+        int at = row * KB + place_of<KB, SPREAD>(row, l >> 4) * 16;
+        asm volatile("" : "+v"(at));   // (one register, not one for every place that it is added to)
+        return at;
     }
+    static constexpr int on(int f) { return SPREAD == 1 ? f * 16 * KB : (f / SPREAD * 16 * SPREAD + f % SPREAD * 4) * KB; }
+    static __device__ __forceinline__ i32x4 frag(const char* lds, int lane, int f) { return *reinterpret_cast<const i32x4*>(lds + lane + on(f)); }
 };
 
 // ---- KO: rows of COLS values, a row for each value of K in a step of 64 bytes of K
@@ -179,27 +185,84 @@ struct StageKO {
 #pragma unroll
         for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + (t * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16) = held[t];
     }
-    // fragment of the 16 columns from col (a multiple of 16) on
-    static __device__ __forceinline__ i32x4 frag(const char* lds, int col) {
-        const int l = (int)(threadIdx.x & 63), g = l >> 4;
+    // Where this lane reads for the fragment of the 16 columns from col (a multiple of 16) on.  16-bit: 16 lanes give the addresses of 4 x 16 numbers, four
+    // lanes a row, and receive a column each; the other four of a lane's eight values of K lie four rows on, under the same key.  32-bit: the lane's first value of K;
+    // the others lie in the rows behind it, under the same key.
+    static __device__ __forceinline__ int lane(int col) {
+        const int l = (int)threadIdx.x & 63, g = l >> 4;
+        int at;
         if (sizeof(T) == 2) {
-            // 16 lanes give the addresses of 4 x 16 numbers, four lanes a row, and receive a column each
+            const int k = 8 * g + ((l & 15) >> 2), c = col * 2 + (l & 3) * 8;
+            at = k * ROW + group_at(k, c >> 4) * 16 + (c & 8);
+        } else {
+            const int k = 4 * g, c = (col + (l & 15)) * 4;
+            at = k * ROW + group_at(k, c >> 4) * 16 + (c & 15);
+        }
+        asm volatile("" : "+v"(at));
+        return at;
+    }
+    static __device__ __forceinline__ i32x4 frag(const char* lds, int lane) {
+        if (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) i16x4 lds4;
-            const int k = 8 * g + ((l & 15) >> 2), at = col * 2 + (l & 3) * 8;
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + k * ROW + group_at(k, at >> 4) * 16 + (at & 8)));
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + (k + 4) * ROW + group_at(k + 4, at >> 4) * 16 + (at & 8)));
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + lane));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + lane + 4 * ROW));
             return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         i32x4 r;
-        const int at = (col + (l & 15)) * 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = 4 * g + j;
-            r[j] = *reinterpret_cast<const int*>(lds + k * ROW + group_at(k, at >> 4) * 16 + (at & 15));
-        }
+        for (int j = 0; j < 4; ++j) r[j] = *reinterpret_cast<const int*>(lds + lane + j * ROW);
         return r;
     }
 };
+
+// ---- the walk along K
+// Fragments of a step are read in a first set of X, which every product of the step uses, and GROUPS of Y.  A group is read while the one before it is being
+// multiplied, and the next step's first ones during the last group's products: a wavefront that has read the last group says so by the barrier, behind which the
+// next step is there for all, and this step's place is free for step s + STAGES.
+//   arrive(s): this wavefront's part of step s has landed; ask(s): step s is asked for, if there is one; first(s, x), group(s, g, y): fragments; multiply(g, x, y)
+template <int X, int GROUPS, int Y, int STAGES, typename Arrive, typename Ask, typename First, typename Group, typename Multiply>
+__device__ __forceinline__ void walk(int steps, Arrive arrive, Ask ask, First first, Group group, Multiply multiply) {
+    static_assert(GROUPS > 1, "a group is read while another is multiplied");
+    i32x4 xa[X], xb[X], ya[Y], yb[Y];
+    auto step = [&](int s, i32x4 (&x)[X], i32x4 (&xn)[X], i32x4 (&y)[Y], i32x4 (&yn)[Y]) {   // y holds the first group
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            i32x4 (&now)[Y] = g & 1 ? yn : y, (&then)[Y] = g & 1 ? y : yn;
+            if (g + 1 < GROUPS) group(s, g + 1, then);
+            else {   // (behind the last step too: what is read there is in LDS, and is not used; a branch would cost registers)
+                arrive(s + 1);
+                __syncthreads();
+                first(s + 1, xn);
+                group(s + 1, 0, then);
+                ask(s + STAGES);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(g, x, now);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) ask(s);
+    arrive(0);
+    __syncthreads();
+    first(0, xa);
+    group(0, 0, ya);
+    // the next step's first group is in y if the groups are even, else in yn
+    int s = 0;
+    for (; s + 2 <= steps; s += 2) {
+        step(s, xa, xb, ya, yb);
+        if (GROUPS % 2) step(s + 1, xb, xa, yb, ya);
+        else step(s + 1, xb, xa, ya, yb);
+    }
+    if (s < steps) step(s, xa, xb, ya, yb);
+}
+// ... of which a wavefront asks for LOADS pieces a step: waits for step s, where all that may be are behind it
+template <int STAGES, int LOADS>
+__device__ __forceinline__ void arrived(int s, int steps) {
+    if (s == 0 && steps >= STAGES) landed<(STAGES - 1) * LOADS>();
+    else if (s > 0 && s + STAGES - 1 <= steps) landed<(STAGES - 2) * LOADS>();   // (step s + STAGES - 1 is asked for behind the barrier)
+    else landed<0>();
+}
 
 // ---- the block's activations
 // 1 / (1 + exp(-a)), by the hardware's exponential and reciprocal (each off by one unit in the last place; the exponent's rounding adds |a| of them to the

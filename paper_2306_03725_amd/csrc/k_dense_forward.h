@@ -61,11 +61,12 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
 }
 
 // A tile of BD activations of BB instances.  DIRECT: rows and bases are multiples of 16 bytes; STAGES steps of K then have room in LDS, one being
-// multiplied and the others on their way.  Else the tiles come through registers, two steps ahead.
+// multiplied and the others on their way.  Else the tiles come through registers, asked for two steps ahead.
 template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
 __global__ void __launch_bounds__(64 * WAVES_D * WAVES_B, 2)   // (two wavefronts to a SIMD: sums and fragments in 256 registers)
 k_dense_forward(Forward a) {
-    constexpr int WAVES = WAVES_D * WAVES_B, KB = 64, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16, AHEAD = STAGES - 1;
+    constexpr int WAVES = WAVES_D * WAVES_B, KB = 64, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16;
+    static_assert(DIRECT || STAGES == 2, "two sets of registers");
     using Acc = typename Core<T>::Acc;
     using SV = StageKC<BD, KB, FD, WAVES>;   // (a lane's neighbours of all fragments are neighbours)
     using SE = StageKC<BB, KB, 1, WAVES>;
@@ -89,43 +90,53 @@ k_dense_forward(Forward a) {
 #pragma unroll
             for (int h = 0; h < FB; ++h) acc[q][f][h] = Acc{0, 0, 0, 0};
     const int steps = (a.row_bytes + KB - 1) / KB;
-    auto multiply = [&](const char* from) {
-        i32x4 eb[FB];
-#pragma unroll
-        for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + MATS * SV::BYTES, wb, f, 0);
-#pragma unroll
-        for (int q = 0; q < MATS; ++q)
-#pragma unroll
-            for (int f = 0; f < FD; ++f) {
-                const i32x4 v = SV::frag(from + q * SV::BYTES, wd, f, 0);
-#pragma unroll
-                for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
-            }
-    };
+    const int lane_v = SV::lane(wd), lane_e = SE::lane(wb);
     if constexpr (DIRECT) {
-        auto ask = [&](int s, int place) {
-            const int at = s * KB, left = a.row_bytes - at;
-            const uint32_t to = lds_at(lds + place * STEP);
+        constexpr int GROUPS = 2, Y = MATS * FD / GROUPS;   // a matrix, or half of one's fragments
+        auto place = [&](int s) { return lds + s % STAGES * STEP; };
+        walk<FB, GROUPS, Y, STAGES>(
+            steps, [&](int s) { arrived<STAGES, LOADS>(s, steps); },
+            [&](int s) {
+                if (s >= steps) return;
+                const int at = s * KB, left = a.row_bytes - at;
+                const uint32_t to = lds_at(place(s));
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) SV::direct(to + q * SV::BYTES, V[q] + at, rows_d, pitch, left);
-            SE::direct(to + MATS * SV::BYTES, e + at, rows_b, pitch, left);
-        };
+                for (int q = 0; q < MATS; ++q) SV::direct(to + q * SV::BYTES, V[q] + at, rows_d, pitch, left);
+                SE::direct(to + MATS * SV::BYTES, e + at, rows_b, pitch, left);
+            },
+            [&](int s, i32x4 (&x)[FB]) {
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s)
-            if (s < steps) ask(s, s);
-        int here = 0, next = AHEAD;   // step s's place, and that of step s + AHEAD (where step s - 1 was)
-        for (int s = 0; s < steps; ++s) {
-            if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();   // step s, but for the steps behind it
-            else landed<0>();
-            __syncthreads();   // for all wavefronts, and nobody reads step s - 1 any more
-            if (s + AHEAD < steps) ask(s + AHEAD, next);
-            multiply(lds + here * STEP);
-            here = here + 1 == STAGES ? 0 : here + 1;
-            next = next + 1 == STAGES ? 0 : next + 1;
-        }
+                for (int f = 0; f < FB; ++f) x[f] = SE::frag(place(s) + MATS * SV::BYTES, lane_e, f);
+            },
+            [&](int s, int g, i32x4 (&y)[Y]) {
+#pragma unroll
+                for (int f = 0; f < Y; ++f) y[f] = SV::frag(place(s) + (g * Y + f) / FD * SV::BYTES, lane_v, (g * Y + f) % FD);
+            },
+            [&](int g, const i32x4 (&x)[FB], const i32x4 (&y)[Y]) {
+#pragma unroll
+                for (int f = 0; f < Y; ++f)
+#pragma unroll
+                    for (int h = 0; h < FB; ++h) {
+                        Acc& to = acc[(g * Y + f) / FD][(g * Y + f) % FD][h];
+                        to = Core<T>::mul(y[f], x[h], to);
+                    }
+            });
     } else {
         struct Held { i32x4 v[MATS][SV::LOADS], e[SE::LOADS]; };
         Held one, two;   // steps s + 1 and s + 2
+        auto multiply = [&](const char* from) {
+            i32x4 eb[FB];
+#pragma unroll
+            for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + MATS * SV::BYTES, lane_e, f);
+#pragma unroll
+            for (int q = 0; q < MATS; ++q)
+#pragma unroll
+                for (int f = 0; f < FD; ++f) {
+                    const i32x4 v = SV::frag(from + q * SV::BYTES, lane_v, f);
+#pragma unroll
+                    for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
+                }
+        };
         auto ask = [&](Held& h, int s) {
             if (s >= steps) return;
             const int at = s * KB, left = a.row_bytes - at;
@@ -156,7 +167,7 @@ k_dense_forward(Forward a) {
         }
     }
     constexpr int N = 4 * FD, WD = BD / WAVES_D;
-    static_assert(WAVES * 16 * (WD * (int)sizeof(TO) + 16) <= (DIRECT ? STAGES : 2) * STEP, "room for the outputs");
+    static_assert(WAVES * 16 * (WD * (int)sizeof(TO) + 16) <= STAGES * STEP, "room for the outputs");
     const int l = (int)threadIdx.x & 63, i0 = b0 + wb, c0 = d0 + wd;
     char* mine = lds + wave * 16 * (WD * (int)sizeof(TO) + 16);
     Scales<T, MATS, N> scales;
@@ -252,7 +263,7 @@ k_dense_few(Forward a) {
 
 template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
 usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
-    constexpr int BYTES = (DIRECT ? STAGES : 2) * (MATS * BD + BB) * 64;
+    constexpr int BYTES = STAGES * (MATS * BD + BB) * 64;
     const auto kernel = k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, STAGES, DIRECT>;
     a.tiles_d = (a.d + BD - 1) / BD;
     a.tiles_b = (a.b + BB - 1) / BB;

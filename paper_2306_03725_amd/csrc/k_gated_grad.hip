@@ -4,7 +4,8 @@
 //   grad_e = G_gate V_gate + G_up V_up,  grad_V_gate = G_gate^T e,  grad_V_up = G_up^T e
 //
 // The instances go through in chunks; for each, a first launch writes G = [G_gate | G_up] and a copy of e whose rows are padded with zeros, then two products
-// (k_dense.h).  With bfloat16 storage G, a product of float32 numbers, is the exact sum of three bfloat16 ones (8 + 8 + 8 bits, cut off, not rounded), and each
+// (k_dense.h).  G lies in blocks of 128 columns, the instances one behind the other: with whole rows, a power of two apart, a tile's 32 or 128 rows met in
+// one channel of the caches.  With bfloat16 storage G, a product of float32 numbers, is the exact sum of three bfloat16 ones (8 + 8 + 8 bits, cut off, not rounded), and each
 // product is three on the matrix cores that share their other operand: gradients are float32 numbers, and G rounded to bfloat16 would leave them 1e-3 off, two parts 2e-6.
 #include "k_dense.h"
 
@@ -20,7 +21,7 @@ struct Grad {
     const float* grad_x;
     const void *e, *V[2], *gate, *up;
     float *grad_e, *grad_V[2];
-    char *G, *E;               // chunk: [parts][rows][2 * dp], [rows][wp]
+    char *G, *E;               // chunk: [parts][2 * dp / 128][rows][128], [rows][wp]
     float* sums;               // [splits][rows][w]
     int d, w, dp, wp, b;       // b: instances of this chunk
     int rows;                  // padded instances of the chunk
@@ -107,7 +108,7 @@ k_gated_slopes(Grad a) {
             by_up[j] = g[j] * value;
         }
     }
-    T* to = (T*)a.G + (size_t)i * 2 * a.dp + c;
+    T* to = (T*)a.G + ((size_t)(c >> 7) * a.rows + i) * 128 + (c & 127);
     const size_t next = (size_t)a.rows * 2 * a.dp;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
@@ -120,70 +121,72 @@ k_gated_slopes(Grad a) {
             for (int q = 0; q < PARTS<T>; ++q) v[q].v[j] = part[q];
         }
 #pragma unroll
-        for (int q = 0; q < PARTS<T>; ++q) store(to + q * next + side * a.dp, v[q]);
+        for (int q = 0; q < PARTS<T>; ++q) store(to + q * next + (size_t)side * a.dp * a.rows, v[q]);
     }
 }
 
-// One of so many tiles: workgroups go to the chiplets in turn, and the `inner` tiles of an outer one, which share what they read, go to one chiplet together.
-__device__ __forceinline__ void tile_of(int inner, int& in, int& out) {
-    const int turn = (int)blockIdx.x >> 3;
-    in = turn % inner;
-    out = turn / inner * 8 + ((int)blockIdx.x & 7);
+// One of `inner` tiles of one of `outer` pieces.  Workgroups go to the chiplets in turn; each of those takes a run of tiles, so that those of a piece, which share
+// what they read, meet in its cache.  false: one too many
+__device__ __forceinline__ bool tile_of(int inner, int outer, int& in, int& out) {
+    const int each = (inner * outer + 7) / 8, at = ((int)blockIdx.x & 7) * each + ((int)blockIdx.x >> 3);
+    in = at % inner;
+    out = at / inner;
+    return out < outer;
 }
-unsigned tiles_grid(int inner, int outer) { return (unsigned)((outer + 7) / 8 * 8 * inner); }
+unsigned tiles_grid(int inner, int outer) { return (unsigned)((inner * outer + 7) / 8 * 8); }
 
 // grad_V: [w] along m, [2][d] along n, the instances along K.  Tiles of MT x 128, a wavefront 64 x 64 of it.  The parts of G meet the same fragments of e, so
 // what has to come from the caches for a product on the matrix cores falls with MT.
 template <typename T, int MT, int STAGES>
 __global__ void __launch_bounds__(2 * MT, 2)
 k_gated_grad_v(Grad a) {
-    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 32, AHEAD = STAGES - 1;
+    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 32;
     using SE = StageKO<T, MT, WAVES>;
     using SG = StageKO<T, 128, WAVES>;
     constexpr int STEP = SE::BYTES + P * SG::BYTES, LOADS = SE::LOADS + P * SG::LOADS;
     extern __shared__ __align__(1024) char lds[];
     int tm, tn;
-    tile_of(a.tiles_m, tm, tn);
-    if (tn >= 2 * a.dp / 128) return;
+    if (!tile_of(a.tiles_m, 2 * a.dp / 128, tm, tn)) return;
     const int m0 = tm * MT, n0 = tn * 128, wave = (int)threadIdx.x >> 6, wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-    const size_t pitch_e = (size_t)a.wp * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next_part = a.rows * pitch_g;
-    const char *E = a.E + (size_t)m0 * sizeof(T), *G = a.G + (size_t)n0 * sizeof(T);
+    const size_t pitch_e = (size_t)a.wp * sizeof(T), pitch_g = 128 * sizeof(T), next_part = (size_t)a.rows * 2 * a.dp * sizeof(T);
+    const char *E = a.E + (size_t)m0 * sizeof(T), *G = a.G + (size_t)tn * a.rows * pitch_g;
     f32x4 acc[F][F];
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int h = 0; h < F; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
     const int steps = a.rows / SE::DEPTH;
-    auto ask = [&](int s, int place) {
-        const uint32_t to = lds_at(lds + place * STEP);
-        SE::direct(to, E + (size_t)s * SE::DEPTH * pitch_e, SE::DEPTH, pitch_e, SE::ROW);
+    int lane_e[F], lane_g[F];
 #pragma unroll
-        for (int q = 0; q < P; ++q) SG::direct(to + SE::BYTES + q * SG::BYTES, G + q * next_part + (size_t)s * SE::DEPTH * pitch_g, SE::DEPTH, pitch_g, SG::ROW);
-    };
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
-        if (s < steps) ask(s, s);
-    int here = 0, next = AHEAD;
-    for (int s = 0; s < steps; ++s) {
-        if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();
-        else landed<0>();
-        __syncthreads();   // step s is there, and nobody reads step s - 1 any more
-        if (s + AHEAD < steps) ask(s + AHEAD, next);
-        const char* from = lds + here * STEP;
-        i32x4 x[F];
-#pragma unroll
-        for (int f = 0; f < F; ++f) x[f] = SE::frag(from, wm + f * 16);
-#pragma unroll
-        for (int q = P - 1; q >= 0; --q)   // the small parts first
-#pragma unroll
-            for (int h = 0; h < F; ++h) {
-                const i32x4 y = SG::frag(from + SE::BYTES + q * SG::BYTES, wn + h * 16);
-#pragma unroll
-                for (int f = 0; f < F; ++f) acc[f][h] = Core<T>::mul(x[f], y, acc[f][h]);
-            }
-        here = here + 1 == STAGES ? 0 : here + 1;
-        next = next + 1 == STAGES ? 0 : next + 1;
+    for (int f = 0; f < F; ++f) {
+        lane_e[f] = SE::lane(wm + f * 16);
+        lane_g[f] = SG::lane(wn + f * 16);
     }
+    auto place = [&](int s) { return lds + s % STAGES * STEP; };
+    constexpr int GROUPS = P > 1 ? P : 2, Y = P * F / GROUPS;   // a part, or half of the only one; the small parts first
+    walk<F, GROUPS, Y, STAGES>(
+        steps, [&](int s) { arrived<STAGES, LOADS>(s, steps); },
+        [&](int s) {
+            if (s >= steps) return;
+            const uint32_t to = lds_at(place(s));
+            SE::direct(to, E + (size_t)s * SE::DEPTH * pitch_e, SE::DEPTH, pitch_e, SE::ROW);
+#pragma unroll
+            for (int q = 0; q < P; ++q) SG::direct(to + SE::BYTES + q * SG::BYTES, G + q * next_part + (size_t)s * SE::DEPTH * pitch_g, SE::DEPTH, pitch_g, SG::ROW);
+        },
+        [&](int s, i32x4 (&x)[F]) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) x[f] = SE::frag(place(s), lane_e[f]);
+        },
+        [&](int s, int g, i32x4 (&y)[Y]) {
+#pragma unroll
+            for (int h = 0; h < Y; ++h) y[h] = SG::frag(place(s) + SE::BYTES + (P - 1 - (g * Y + h) / F) * SG::BYTES, lane_g[(g * Y + h) % F]);
+        },
+        [&](int g, const i32x4 (&x)[F], const i32x4 (&y)[Y]) {
+#pragma unroll
+            for (int h = 0; h < Y; ++h)
+#pragma unroll
+                for (int f = 0; f < F; ++f) acc[f][(g * Y + h) % F] = Core<T>::mul(x[f], y[h], acc[f][(g * Y + h) % F]);
+        });
     const int l = (int)threadIdx.x & 63;
 #pragma unroll
     for (int h = 0; h < F; ++h) {
@@ -208,17 +211,16 @@ k_gated_grad_v(Grad a) {
 template <typename T, int MT, int NT, int STAGES, bool DIRECT>
 __global__ void __launch_bounds__(MT * NT / 64, 2)
 k_gated_grad_e(Grad a) {
-    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / 64), AHEAD = STAGES - 1;
-    static_assert(DIRECT || STAGES == 3, "two steps ahead through registers");
+    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / 64);
     using SV = StageKO<T, MT, WAVES>;
     using SG = StageKC<NT, 64, 1, WAVES>;
-    constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (DIRECT ? SV::LOADS : 0) + P * SG::LOADS;   // (loads into registers only make a wait longer)
+    constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (DIRECT ? SV::LOADS : 0) + P * SG::LOADS;
+    static_assert(DIRECT || STAGES == 3, "two steps ahead");
     extern __shared__ __align__(1024) char lds[];
     int tile, piece;
-    tile_of(a.tiles_m * a.tiles_n, tile, piece);
-    if (piece >= a.splits) return;
+    if (!tile_of(a.tiles_m * a.tiles_n, a.splits, tile, piece)) return;
     const int m0 = tile % a.tiles_m * MT, n0 = tile / a.tiles_m * NT, wave = (int)threadIdx.x >> 6, wm = wave % (MT / 64) * 64, wn = wave / (MT / 64) * 64;
-    const size_t pitch_v = (size_t)a.w * sizeof(T), pitch_g = (size_t)2 * a.dp * sizeof(T), next_part = a.rows * pitch_g;
+    const size_t pitch_v = (size_t)a.w * sizeof(T), pitch_g = 128 * sizeof(T), next_part = (size_t)a.rows * 2 * a.dp * sizeof(T);
     const int rows = a.rows - n0;   // (those behind the last instance hold zeros)
     f32x4 acc[F][F];
 #pragma unroll
@@ -226,61 +228,76 @@ k_gated_grad_e(Grad a) {
 #pragma unroll
         for (int h = 0; h < F; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
     const int first = piece * a.steps_each, steps = min(a.steps_each, 2 * a.dp / SV::DEPTH - first);
-    struct Held { i32x4 v[SV::LOADS]; };
-    Held one, two;
-    auto ask = [&](int s, int place) {
+    int lane_v[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) lane_v[f] = SV::lane(wm + f * 16);
+    const int lane_g = SG::lane(wn);
+    auto place = [&](int s) { return lds + s % STAGES * STEP; };
+    auto ask_g = [&](int s) {
+        if (s >= steps) return;
         const int k = (first + s) * SV::DEPTH;
-        const uint32_t to = lds_at(lds + place * STEP);
 #pragma unroll
         for (int q = 0; q < P; ++q)
-            SG::direct(to + SV::BYTES + q * SG::BYTES, a.G + q * next_part + (size_t)n0 * pitch_g + (size_t)k * sizeof(T), rows, (uint32_t)pitch_g, 64);
+            SG::direct(lds_at(place(s) + SV::BYTES + q * SG::BYTES), a.G + q * next_part + ((size_t)(k >> 7) * a.rows + n0) * pitch_g + (size_t)(k & 127) * sizeof(T), rows,
+                       (uint32_t)pitch_g, 64);
     };
-    auto matrix = [&](int s, int place, Held& h) {
+    struct Held { i32x4 v[SV::LOADS]; };
+    auto ask_v = [&](int s, Held* h) {
         if (s >= steps) return;
         const int k = (first + s) * SV::DEPTH, which = k >= a.dp, row = k - which * a.dp;   // rows behind V's end meet zeros of G, and are not read
         const char* V = (const char*)a.V[which] + (size_t)min(row, a.d - 1) * pitch_v + (size_t)m0 * sizeof(T);
-        if constexpr (DIRECT) SV::direct(lds_at(lds + place * STEP), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
-        else SV::fetch(h.v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
+        if constexpr (DIRECT) SV::direct(lds_at(place(s)), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
+        else SV::fetch(h->v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
     };
-    auto multiply = [&](const char* from) {
-        i32x4 x[F];
+    constexpr int GROUPS = P > 1 ? P : 2, Y = P * F / GROUPS;
+    auto first_of = [&](int s, i32x4 (&x)[F]) {
 #pragma unroll
-        for (int f = 0; f < F; ++f) x[f] = SV::frag(from, wm + f * 16);
+        for (int f = 0; f < F; ++f) x[f] = SV::frag(place(s), lane_v[f]);
+    };
+    auto group_of = [&](int s, int g, i32x4 (&y)[Y]) {
 #pragma unroll
-        for (int q = P - 1; q >= 0; --q)
+        for (int h = 0; h < Y; ++h) y[h] = SG::frag(place(s) + SV::BYTES + (P - 1 - (g * Y + h) / F) * SG::BYTES, lane_g, (g * Y + h) % F);
+    };
+    auto multiply = [&](int g, const i32x4 (&x)[F], const i32x4 (&y)[Y]) {
 #pragma unroll
-            for (int h = 0; h < F; ++h) {
-                const i32x4 y = SG::frag(from + SV::BYTES + q * SG::BYTES, wn, h, 0);
+        for (int h = 0; h < Y; ++h)
 #pragma unroll
-                for (int f = 0; f < F; ++f) acc[f][h] = Core<T>::mul(x[f], y, acc[f][h]);
+            for (int f = 0; f < F; ++f) acc[f][(g * Y + h) % F] = Core<T>::mul(x[f], y[h], acc[f][(g * Y + h) % F]);
+    };
+    if constexpr (DIRECT) {
+        walk<F, GROUPS, Y, STAGES>(
+            steps, [&](int s) { arrived<STAGES, LOADS>(s, steps); },
+            [&](int s) {
+                ask_v(s, nullptr);
+                ask_g(s);
+            },
+            first_of, group_of, multiply);
+    } else {
+        Held one, two;
+        auto turn = [&](int s, Held& after, Held& behind) {   // after: V of step s + 1; behind: to hold that of step s + 2
+            if (s + 2 <= steps) landed<LOADS>();   // (G of step s + 1 may be on its way; loads into registers behind it only make the wait longer)
+            else landed<0>();
+            __syncthreads();
+            ask_g(s + 2);
+            ask_v(s + 2, &behind);
+            i32x4 x[F], y[Y];
+            first_of(s, x);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                group_of(s, g, y);
+                multiply(g, x, y);
             }
-    };
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
-        if (s < steps) {
-            ask(s, s);
-            if (DIRECT) matrix(s, s, one);
-        }
-    int here = 0, next = AHEAD;
-    auto turn = [&](int s, Held& after, Held& behind) {   // after: V of step s + 1; behind: to hold that of step s + 2
-        if (s + AHEAD <= steps) landed<(AHEAD - 1) * LOADS>();
-        else landed<0>();
-        __syncthreads();
-        if (s + AHEAD < steps) ask(s + AHEAD, next);
-        matrix(s + AHEAD, next, behind);
-        multiply(lds + here * STEP);
-        here = here + 1 == STAGES ? 0 : here + 1;
-        next = next + 1 == STAGES ? 0 : next + 1;
-        if (!DIRECT && s + 1 < steps) SV::put(lds + here * STEP, after.v);
-    };
-    if constexpr (!DIRECT) {
-        matrix(0, 0, two);
-        matrix(1, 1, one);
+            if (s + 1 < steps) SV::put(place(s + 1), after.v);
+        };
+        ask_g(0);
+        ask_g(1);
+        ask_v(0, &two);
+        ask_v(1, &one);
         SV::put(lds, two.v);
-    }
-    for (int s = 0; s < steps; s += 2) {
-        turn(s, one, two);
-        if (s + 1 < steps) turn(s + 1, two, one);
+        for (int s = 0; s < steps; s += 2) {
+            turn(s, one, two);
+            if (s + 1 < steps) turn(s + 1, two, one);
+        }
     }
     const int l = (int)threadIdx.x & 63;
     float* sums = a.sums + (size_t)piece * a.b * a.w;
