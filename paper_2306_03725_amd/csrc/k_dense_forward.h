@@ -26,10 +26,12 @@ struct Scales {
                 for (int j = 0; j < N; ++j) v[q][j] = a.V_scale[q][min(d0 + j, a.d - 1)];
     }
 };
+// gate and up go past the caches, which have V and e to keep: 512 x 768 -> 32768 bfloat16 74 us, so 67 (x too: 68); the results from 8-bit integers too: 1024 x 512 ->
+// 65536 67 and 59, 500 x 750 -> 32768 gated 60 and 58.
 // 16 instances' values of WD neighbouring activations, a lane N of one instance's, to rows of memory: through LDS, so that a store takes whole lines of it.
 // (16 rows of 64 bytes to a store, the other half of every line by the next one: 512 x 768 -> 32768 bfloat16, three outputs, 85 us, and with more between the
 // two 98; in whole lines 73.)  `mine`: the wavefront's own LDS.
-template <typename TO, int WD, int N>
+template <typename TO, int WD, bool PAST_CACHES, int N>
 __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N], int i0, int b, int d0, int d) {
     constexpr int ROW = WD * (int)sizeof(TO), PITCH = ROW + 16, EACH = 16 / (int)sizeof(TO), GROUPS = ROW / 16;
     static_assert(N * 4 == WD, "four lanes share a row");
@@ -49,7 +51,8 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
         TO* p = to + (size_t)i * d + c;
         if (d - c >= EACH) {
             typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
-            *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
+            if (PAST_CACHES) __builtin_nontemporal_store(__builtin_bit_cast(Words, w), reinterpret_cast<Words*>(p));
+            else *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
         } else {
             TO one[EACH];
             __builtin_memcpy(one, &w, 16);
@@ -185,15 +188,15 @@ k_dense_forward(Forward a) {
                 if (sizeof(T) == 1) v[q][j] *= e_scale * scales.v[q][j];
             }
         if (MATS == 1) {
-            put_tile<TO, WD, N>(mine, (TO*)a.x, v[0], i0 + g * 16, a.b, c0, a.d);
+            put_tile<TO, WD, true>(mine, (TO*)a.x, v[0], i0 + g * 16, a.b, c0, a.d);
             continue;
         }
         float x[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
-        put_tile<TO, WD, N>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d);
-        if (a.gate) put_tile<TO, WD, N>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d);
-        if (a.up) put_tile<TO, WD, N>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d);
+        put_tile<TO, WD, sizeof(T) == 1>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d);
+        if (a.gate) put_tile<TO, WD, true>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d);
+        if (a.up) put_tile<TO, WD, true>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d);
     }
 }
 

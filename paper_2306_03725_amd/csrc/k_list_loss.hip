@@ -78,6 +78,23 @@ template <typename T> __device__ __forceinline__ T block_join(T v, bool largest,
     return r;
 }
 
+template <int N>   // the same for N sums at a time; red holds N * LL_NT / 64 values
+__device__ __forceinline__ void block_sums(double (&v)[N], double* red) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] = wave_join(v[q], false);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+        if ((threadIdx.x & 63) == 0) red[q * (LL_NT / 64) + (threadIdx.x >> 6)] = v[q];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        v[q] = red[q * (LL_NT / 64)];
+#pragma unroll
+        for (int w = 1; w < LL_NT / 64; ++w) v[q] += red[q * (LL_NT / 64) + w];
+    }
+}
+
 __global__ void __launch_bounds__(LL_NT)
 k_list_parts(Lists a, Part* __restrict__ parts) {
     __shared__ float red[LL_NT / 64];
@@ -121,11 +138,24 @@ __device__ __forceinline__ float score_of(const Lists& a, const float* row, int3
     counts = inside && !(z == -INFINITY);
     return z;
 }
+// A lane's first entry, asked for before the row's sum is known; lists are seldom longer than the workgroup
+template <bool TEACHER>
+struct Entry {
+    float z, value;   // value: the teacher's logit
+    bool counts;
+    __device__ __forceinline__ void load(const Lists& a, const float* row, int64_t e) {
+        z = score_of(a, row, a.lab[e], counts);
+        if (TEACHER) {
+            value = a.logit[e];
+            counts = counts && !(value * a.inv_t == -INFINITY);
+        }
+    }
+};
 
 template <bool TEACHER>
 __global__ void __launch_bounds__(LL_NT)
 k_list_rows(Lists a, const Part* __restrict__ parts, Row* __restrict__ rows, double* __restrict__ row_loss) {
-    __shared__ double red[LL_NT / 64];
+    __shared__ double red[3 * LL_NT / 64];
     const int i = (int)blockIdx.x, tid = (int)threadIdx.x;
     const int64_t p0 = a.off[i], n = a.off[i + 1] - p0;
     if (n <= 0) {
@@ -137,63 +167,73 @@ k_list_rows(Lists a, const Part* __restrict__ parts, Row* __restrict__ rows, dou
     }
     const float* row = a.out + (int64_t)i * a.m;
     parts += (size_t)i * a.nseg;
-    double best = -INFINITY;
-    for (int s = tid; s < a.nseg; s += LL_NT) best = fmax(best, (double)parts[s].top);
+    const Part held = parts[min(tid, a.nseg - 1)];
+    Entry<TEACHER> own;
+    own.load(a, row, p0 + min((int64_t)tid, n - 1));
+    own.counts = own.counts && tid < n;
+    double best = tid < a.nseg ? (double)held.top : -INFINITY;
+    for (int s = tid + LL_NT; s < a.nseg; s += LL_NT) best = fmax(best, (double)parts[s].top);
     best = block_join(best, true, red);
     const float top = (float)best, from = shift_of(top);
-    double sum = 0.0;
-    for (int s = tid; s < a.nseg; s += LL_NT) {
-        const Part p = parts[s];
-        sum += p.top == -INFINITY && p.sum == 0.f ? 0.0 : (double)p.sum * exp(((double)shift_of(p.top) - (double)from) * (double)a.inv_t);
-    }
-    sum = block_join(sum, false, red);
-    const double log_sum = log(sum);
+    auto share = [&](const Part& p) {
+        return p.top == -INFINITY && p.sum == 0.f ? 0.0 : (double)p.sum * exp(((double)shift_of(p.top) - (double)from) * (double)a.inv_t);
+    };
+    double sum = tid < a.nseg ? share(held) : 0.0;
+    for (int s = tid + LL_NT; s < a.nseg; s += LL_NT) sum += share(parts[s]);
     double total = 0.0, loss = 0.0, teacher = 0.0, count = 0.0;
+    // every entry of this lane's, the first one from registers
+    auto each = [&](auto what) {
+        if (own.counts) what(own, p0 + tid);
+        for (int64_t e = p0 + tid + LL_NT; e < p0 + n; e += LL_NT) {
+            Entry<TEACHER> one;
+            one.load(a, row, e);
+            if (one.counts) what(one, e);
+        }
+    };
+    double log_sum;
     if (TEACHER) {
         double most = -INFINITY;
-        for (int64_t e = p0 + tid; e < p0 + n; e += LL_NT) {
-            bool counts;
-            (void)score_of(a, row, a.lab[e], counts);
-            const double t = (double)a.logit[e] * (double)a.inv_t;
-            if (counts && !(t == -INFINITY)) {
-                count += 1.0;
-                most = t > most ? t : most;
-            }
-        }
+        each([&](const Entry<TEACHER>& v, int64_t) {
+            const double t = (double)v.value * (double)a.inv_t;
+            most = t > most ? t : most;
+            count += 1.0;
+        });
         most = block_join(most, true, red);
-        double mass = 0.0, cross = 0.0;
-        for (int64_t e = p0 + tid; e < p0 + n; e += LL_NT) {
-            bool counts;
-            const float z = score_of(a, row, a.lab[e], counts);
-            const double t = (double)a.logit[e] * (double)a.inv_t;
-            if (counts && !(t == -INFINITY)) {
-                const double p = exp(t - most);
-                mass += p;
-                cross += p * ((t - most) - ((double)z - (double)from) * (double)a.inv_t);
-            }
-        }
-        mass = block_join(mass, false, red);
-        cross = block_join(cross, false, red);
-        count = block_join(count, false, red);
-        teacher = most + log(mass);
+        double cross = 0.0, mass = 0.0;
+        each([&](const Entry<TEACHER>& v, int64_t) {
+            const double t = (double)v.value * (double)a.inv_t, p = exp(t - most);
+            mass += p;
+            cross += p * ((t - most) - ((double)v.z - (double)from) * (double)a.inv_t);
+        });
+        double joined[3] = {sum, mass, cross};
+        block_sums(joined, red);
+        sum = joined[0];
+        count = (double)__syncthreads_or(count > 0.0);
+        log_sum = log(sum);
+        const double log_mass = log(joined[1]);
+        teacher = most + log_mass;
         total = -a.t;                                                       // of c_e: the p_e add up to 1
-        loss = a.t * a.t * (cross / mass - log(mass) + log_sum);
+        loss = a.t * a.t * (joined[2] / joined[1] - log_mass + log_sum);
     } else {
-        for (int64_t e = p0 + tid; e < p0 + n; e += LL_NT) {
-            bool counts;
-            const float z = score_of(a, row, a.lab[e], counts);
-            const double logp = (double)z - (double)from - log_sum;
-            if (a.logp) a.logp[e] = counts ? (float)logp : -INFINITY;
-            if (counts) {
-                const Slope s = policy_of(a, e, logp);
-                count += 1.0;
-                loss += s.loss;
-                total += s.c;
+        sum = block_join(sum, false, red);
+        log_sum = log(sum);
+        each([&](const Entry<TEACHER>& v, int64_t e) {
+            const Slope s = policy_of(a, e, (double)v.z - (double)from - log_sum);
+            count += 1.0;
+            loss += s.loss;
+            total += s.c;
+        });
+        if (a.logp)
+            for (int64_t e = p0 + tid; e < p0 + n; e += LL_NT) {
+                Entry<TEACHER> one = own;
+                if (e != p0 + tid) one.load(a, row, e);
+                a.logp[e] = one.counts ? (float)((double)one.z - (double)from - log_sum) : -INFINITY;
             }
-        }
-        loss = block_join(loss, false, red);
-        total = block_join(total, false, red);
-        count = block_join(count, false, red);
+        double joined[3] = {loss, total, count};
+        block_sums(joined, red);
+        loss = joined[0];
+        total = joined[1];
+        count = joined[2];
     }
     if (tid == 0) {
         const bool any = count > 0.0;
@@ -227,21 +267,19 @@ k_list_grad(Lists a, const Row* __restrict__ rows, const double* __restrict__ ro
     const int i = (int)blockIdx.y, tid = (int)threadIdx.x;
     const int64_t seg0 = (int64_t)blockIdx.x * LL_SEG;
     const int lim = (int)min((int64_t)LL_SEG, a.m - seg0);
-    const Row r = rows[i];
     const float* row = a.out + (int64_t)i * a.m;
     float v[LL_EPT];
+    const Row r = rows[i];
     if (r.any) {
+        load_segment(row + seg0, lim, v);   // (asked for before the row's sums are there, rows without entries would be read too: 256 x 500k 267 us, with them 280)
         const int64_t p0 = a.off[i], n = a.off[i + 1] - p0;
-        load_segment(row + seg0, lim, v);
         auto here = [&](int32_t label) { return (uint32_t)label - (uint32_t)seg0 < (uint32_t)lim; };
         auto slope = [&](int64_t e) {   // c_e; 0 if the entry does not count
-            bool counts;
-            const float z = score_of(a, row, a.lab[e], counts);
-            if (TEACHER) {
-                const double t = (double)a.logit[e] * (double)a.inv_t;
-                return counts && !(t == -INFINITY) ? -a.t * exp(t - r.teacher) : 0.0;
-            }
-            return counts ? policy_of(a, e, (double)z - (double)r.top - r.log_sum).c : 0.0;
+            Entry<TEACHER> one;
+            one.load(a, row, e);
+            if (!one.counts) return 0.0;
+            if (TEACHER) return -a.t * exp((double)one.value * (double)a.inv_t - r.teacher);
+            return policy_of(a, e, (double)one.z - (double)r.top - r.log_sum).c;
         };
         bool mine = false;
         for (int64_t p = tid; p < n; p += LL_NT) mine |= here(a.lab[p0 + p]);
@@ -295,8 +333,10 @@ k_list_grad(Lists a, const Row* __restrict__ rows, const double* __restrict__ ro
     for (int e = 0; e < LL_EPT; e += 4) {
         const int j = local_label(e);
         if (j + 3 < lim) {
+            // g goes past the caches, which hold scores that this launch has yet to read: 256 x 500k 269 -> 241 us (distillation), 280 -> 256 (policy).  (In
+            // parts of 64 to 172 MB of rows, all three launches for each: 307 to 257; the last rows first: 269.)
             const f32x4 q = {v[e], v[e + 1], v[e + 2], v[e + 3]};
-            *reinterpret_cast<f32x4*>(to + j) = q;
+            __builtin_nontemporal_store(q, reinterpret_cast<f32x4*>(to + j));
         } else {
 #pragma unroll
             for (int u = 0; u < 4; ++u)

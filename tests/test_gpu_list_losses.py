@@ -64,7 +64,8 @@ def distill_case(out, off, lab, logit, T, scale, in_place=False, L=None):
 
 
 SIZES = [(1, 1, [1]), (1, 5, [3]), (3, 64, [0, 10, 1]), (4, 1000, [5, 0, 0, 40]), (2, 4095, [3, 4]), (2, 4096, [3, 4]), (2, 4097, [100, 4]), (5, 8191, [0, 0, 7, 0, 1]),
-         (3, 8193, [1, 300, 2]), (2, 20001, [1000, 64]), (1, 70001, [32]), (70, 3001, [i % 7 for i in range(70)]), (2, 33000, [2000, 1])]
+         (3, 8193, [1, 300, 2]), (2, 20001, [1000, 64]), (1, 70001, [32]), (70, 3001, [i % 7 for i in range(70)]), (2, 33000, [2000, 1]), (3, 65536, [70, 0, 1500]),
+         (2, 65537, [9, 1100]), (300, 1024, [i % 5 for i in range(300)]), (2, 32768, [4, 5000]), (2, 1025, [1025, 3])]
 
 
 @pytest.mark.parametrize("b,m,lengths", SIZES)
@@ -77,9 +78,8 @@ def test_distill(b, m, lengths):
     distill_case(out, off, lab, logit, 3.0, 1.0, in_place=True)
 
 
-def hard_lists():
+def hard_lists(m):
     """Labels twice and often, outside, masked; logits of -infinity; rows where nothing counts, a row without scores."""
-    m = 9000
     gen = torch.Generator().manual_seed(5)
     out = torch.randn(9, m, generator=gen) * 2
     rows = [[3, 3, 3, 8999, 3, 4096, 4095], [-1, m, 2 ** 31 - 1, -2 ** 31, 7], [10, 11], [12, 12, 13], [], [-5, m], [100, 200], [5] * 700 + [6, 5], [20, 20]]
@@ -96,8 +96,9 @@ def hard_lists():
     return out, off, lab, logit, gen
 
 
-def test_distill_of_hard_lists():
-    out, off, lab, logit, _ = hard_lists()
+@pytest.mark.parametrize("wide", [9000, 65537])
+def test_distill_of_hard_lists(wide):
+    out, off, lab, logit, _ = hard_lists(wide)
     for in_place in (False, True):
         g = distill_case(out, off, lab, logit, 1.5, 0.5, in_place=in_place)
         assert bool((g[[2, 4, 5, 6]] == 0).all()) and bool((g[1] != 0).any())
@@ -172,8 +173,9 @@ def test_policy(b, m, lengths):
     policy_case(out, off, lab, old, ref, adv, 1.0, 0.0, 1.0, 0.25, in_place=True)
 
 
-def test_policy_of_hard_lists():
-    out, off, lab, _, gen = hard_lists()
+@pytest.mark.parametrize("wide", [9000, 65537])
+def test_policy_of_hard_lists(wide):
+    out, off, lab, _, gen = hard_lists(wide)
     old, ref, adv = policy_values(out, off, lab, gen)
     last = slice(int(off[8]), int(off[9]))
     old[last] = ref[last] = -1000.0   # (of the label far below the others: the ratio stays a number)
@@ -218,14 +220,15 @@ def test_nothing_is_listed():
     L.close()
 
 
+@pytest.mark.parametrize("m", [9001, 66000])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_scores_that_are_not_numbers(bad):
+def test_scores_that_are_not_numbers(bad, m):
     """NaN or +infinity anywhere in a row that lists an entry: NaN there, and the other rows as without it."""
-    out = torch.randn(3, 9001)
+    out = torch.randn(3, m)
     off, lab = torch.tensor([0, 2, 4, 6]), torch.tensor([1, 2, 3, 4, 5, 6], dtype=torch.int32)
     logit = torch.randn(6)
-    L = layer(9001, 3)
-    clean, dirty, loss = torch.empty(3, 9001, device="cuda"), torch.empty(3, 9001, device="cuda"), torch.empty(1, device="cuda")
+    L = layer(m, 3)
+    clean, dirty, loss = torch.empty(3, m, device="cuda"), torch.empty(3, m, device="cuda"), torch.empty(1, device="cuda")
     L.distill_loss_grad(out.cuda(), off.cuda(), lab.cuda(), logit.cuda(), 1.0, 1.0, clean, loss, 3)
     out[1, 7000] = bad
     L.distill_loss_grad(out.cuda(), off.cuda(), lab.cuda(), logit.cuda(), 1.0, 1.0, dirty, loss, 3)
@@ -271,9 +274,10 @@ def test_gradients_against_differences(kind):
     L.close()
 
 
-def test_batches_in_turn_equal_bits_and_a_graph():
+@pytest.mark.parametrize("m", [10001, 70001])
+def test_batches_in_turn_equal_bits_and_a_graph(m):
     s = torch.cuda.Stream()
-    b, m = 6, 10001
+    b = 6
     off, lab, gen = lists(b, m, [5, 0, 60, 1, 300, 2], 4)
     out = (torch.randn(b, m, generator=gen) * 2).cuda()
     off, lab = off.cuda(), lab.cuda()
