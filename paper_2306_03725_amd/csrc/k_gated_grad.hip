@@ -30,99 +30,94 @@ struct Grad {
     int splits, steps_each;    // of grad_e's sums over d
 };
 
-template <typename T> __device__ __forceinline__ void split(float v, T (&part)[PARTS<T>]);
-template <> __device__ __forceinline__ void split<float>(float v, float (&part)[1]) { part[0] = v; }
-template <> __device__ __forceinline__ void split<bf16>(float v, bf16 (&part)[3]) {
-    const uint32_t u = __float_as_uint(v);
-    if ((u & 0x7F800000u) == 0x7F800000u) {   // an infinity or NaN has no rest
-        part[0] = bf16{usl_f32_to_bf16(v)};
-        part[1] = part[2] = bf16{0};
-        return;
+// Eight neighbours from any address as float32
+typedef uint32_t AnyWords __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void load_eight(const float* p, float (&v)[8]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const AnyWords q = reinterpret_cast<const AnyWords*>(p)[u];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[u * 4 + j] = __uint_as_float(q[j]);
     }
-    const float rest = v - __uint_as_float(u & 0xFFFF0000u);
-    const uint32_t r = __float_as_uint(rest);
-    const float last = rest - __uint_as_float(r & 0xFFFF0000u);
-    part[0] = bf16{(uint16_t)(u >> 16)};
-    part[1] = bf16{(uint16_t)(r >> 16)};
-    part[2] = bf16{(uint16_t)(__float_as_uint(last) >> 16)};
+}
+__device__ __forceinline__ void load_eight(const bf16* p, float (&v)[8]) {
+    const AnyWords q = *reinterpret_cast<const AnyWords*>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j & 1 ? q[j / 2] & 0xFFFF0000u : q[j / 2] << 16);
+}
+// v as the sum of PARTS<T> numbers, each eight to its place: to, to + next, ...
+__device__ __forceinline__ void store_parts(float* to, size_t, const float (&v)[8]) {
+    reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store_parts(bf16* to, size_t next, const float (&v)[8]) {
+    uint32_t rest[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rest[j] = __float_as_uint(v[j]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        uint32_t cut[8];   // the upper half of a word
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            cut[j] = rest[j] & 0xFFFF0000u;
+            const bool odd = (rest[j] & 0x7F800000u) == 0x7F800000u;   // an infinity or NaN has no rest, and a NaN stays one
+            const uint32_t left = __float_as_uint(__uint_as_float(rest[j]) - __uint_as_float(cut[j]));
+            if (q == 0) cut[j] |= odd && (rest[j] & 0x7FFFFFu) ? 0x400000u : 0u;
+            rest[j] = odd ? 0u : left;
+        }
+        uint4 w;
+        w.x = cut[0] >> 16 | cut[1]; w.y = cut[2] >> 16 | cut[3]; w.z = cut[4] >> 16 | cut[5]; w.w = cut[6] >> 16 | cut[7];
+        *reinterpret_cast<uint4*>(to + q * next) = w;
+    }
 }
 
 // G and e's copy, eight columns a lane.  Grid: (groups of 8 columns of G and of e / PREP_NT, rows).  Bound by its bytes.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(PREP_NT)
 k_gated_slopes(Grad a) {
-    constexpr int N = 8;
-    struct Eight { T v[N]; };
-    typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
-    auto load = [](const auto* p, auto& v) {   // from any address
-        Any q[sizeof(v) / 16];
-#pragma unroll
-        for (int u = 0; u < (int)(sizeof(v) / 16); ++u) q[u] = reinterpret_cast<const Any*>(p)[u];
-        __builtin_memcpy(&v, q, sizeof(v));
-    };
-    auto store = [](T* p, const Eight& v) {
-        uint4 q[sizeof(v) / 16];
-        __builtin_memcpy(q, &v, sizeof(v));
-#pragma unroll
-        for (int u = 0; u < (int)(sizeof(v) / 16); ++u) reinterpret_cast<uint4*>(p)[u] = q[u];
-    };
-    const int i = (int)blockIdx.y, groups = a.dp / N;
+    const int i = (int)blockIdx.y, groups = a.dp / 8;
     int c = ((int)blockIdx.x * PREP_NT + (int)threadIdx.x);
     if (c >= groups) {
-        c = (c - groups) * N;
+        c = (c - groups) * 8;
         if (c >= a.wp) return;
-        Eight v;
         const T* e = (const T*)a.e + (size_t)i * a.w + c;
-        if (i < a.b && c + N <= a.w) load(e, v.v);
-        else {
+        T* to = (T*)a.E + (size_t)i * a.wp + c;
+        if (i < a.b && c + 8 <= a.w) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) v.v[j] = i < a.b && c + j < a.w ? e[j] : narrow<T>(0.f);
+            for (int u = 0; u < (int)sizeof(T) / 2; ++u) reinterpret_cast<uint4*>(to)[u] = __builtin_bit_cast(uint4, reinterpret_cast<const AnyWords*>(e)[u]);
+        } else {
+            for (int j = 0; j < 8; ++j) to[j] = i < a.b && c + j < a.w ? e[j] : narrow<T>(0.f);
         }
-        store((T*)a.E + (size_t)i * a.wp + c, v);
         return;
     }
-    c *= N;
-    float by_gate[N], by_up[N];
-    {
-        T gate[N], up[N];
-        float g[N];
-        const size_t at = (size_t)i * a.d + c;
-        if (i < a.b && c + N <= a.d) {
-            load((const T*)a.gate + at, gate);
-            load((const T*)a.up + at, up);
-            load(a.grad_x + at, g);
-        } else {
+    c *= 8;
+    float gate[8], up[8], g[8];
+    const size_t at = (size_t)i * a.d + c;
+    if (i < a.b && c + 8 <= a.d) {
+        load_eight((const T*)a.gate + at, gate);
+        load_eight((const T*)a.up + at, up);
+        load_eight(a.grad_x + at, g);
+    } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const bool is = i < a.b && c + j < a.d;
-                gate[j] = is ? ((const T*)a.gate)[at + j] : narrow<T>(0.f);
-                up[j] = is ? ((const T*)a.up)[at + j] : narrow<T>(0.f);
-                g[j] = is ? a.grad_x[at + j] : 0.f;
-            }
+        for (int j = 0; j < 8; ++j) {
+            const bool is = i < a.b && c + j < a.d;
+            gate[j] = is ? widen(((const T*)a.gate)[at + j]) : 0.f;
+            up[j] = is ? widen(((const T*)a.up)[at + j]) : 0.f;
+            g[j] = is ? a.grad_x[at + j] : 0.f;
         }
+    }
+    float by_up[8];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            float value, slope;
-            act_and_slope<ACT>(widen(gate[j]), value, slope);
-            by_gate[j] = g[j] * widen(up[j]) * slope;
-            by_up[j] = g[j] * value;
-        }
+    for (int j = 0; j < 8; ++j) {
+        float value, slope;
+        act_and_slope<ACT>(gate[j], value, slope);
+        gate[j] = g[j] * up[j] * slope;
+        by_up[j] = g[j] * value;
     }
     T* to = (T*)a.G + ((size_t)(c >> 7) * a.rows + i) * 128 + (c & 127);
     const size_t next = (size_t)a.rows * 2 * a.dp;
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        Eight v[PARTS<T>];
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            T part[PARTS<T>];
-            split<T>(side ? by_up[j] : by_gate[j], part);
-#pragma unroll
-            for (int q = 0; q < PARTS<T>; ++q) v[q].v[j] = part[q];
-        }
-#pragma unroll
-        for (int q = 0; q < PARTS<T>; ++q) store(to + q * next + (size_t)side * a.dp * a.rows, v[q]);
-    }
+    store_parts(to, next, gate);
+    store_parts(to + (size_t)a.dp * a.rows, next, by_up);
 }
 
 // One of `inner` tiles of one of `outer` pieces.  Workgroups go to the chiplets in turn; each of those takes a run of tiles, so that those of a piece, which share
