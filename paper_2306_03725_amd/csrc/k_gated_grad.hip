@@ -382,13 +382,8 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         g.splits = (k_steps + g.steps_each - 1) / g.steps_each;
         return t;
     };
-    size_t sums_most = 0;
-    for (size_t r = 32; r <= most; r += 32) {   // (not always the largest batch's)
-        Grad g = a;
-        cut(g, (int)r);
-        const size_t s = (size_t)g.splits * r * a.w;
-        if (s > sums_most) sums_most = s;
-    }
+    // pieces' sums: no more tiles than compute units, of 128 x 256 at most, or one piece of everything
+    const size_t by_tiles = (size_t)c->num_cu * 128 * 256, sums_most = by_tiles > most * a.w ? by_tiles : most * (size_t)a.w;
     USL_TRY(usl_reserve(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, most * row + sums_most * 4));
     a.G = c->gated_scratch;
     const char *e = (const char*)a.e, *gate = (const char*)a.gate, *up = (const char*)a.up;

@@ -350,8 +350,12 @@ usl_status launch(usl_ctx* c, Lists a, float* g, int32_t b) {
     a.m = c->m;
     a.b = b;
     a.nseg = (int)((c->m + LL_SEG - 1) / LL_SEG);
-    const size_t part_bytes = ((size_t)c->max_b * a.nseg * sizeof(Part) + 255) / 256 * 256, row_bytes = ((size_t)c->max_b * sizeof(Row) + 255) / 256 * 256;
-    USL_TRY(usl_reserve(c, (void**)&c->list_part, &c->list_part_cap, part_bytes + row_bytes + (size_t)c->max_b * sizeof(double)));
+    // for the largest batch that there can be: one of max_b, or of 320 GB of scores
+    int64_t most = ((int64_t)80 << 30) / c->m + 1;
+    if (most > c->max_b) most = c->max_b;
+    if (most < b) most = b;
+    const size_t part_bytes = ((size_t)most * a.nseg * sizeof(Part) + 255) / 256 * 256, row_bytes = ((size_t)most * sizeof(Row) + 255) / 256 * 256;
+    USL_TRY(usl_reserve(c, (void**)&c->list_part, &c->list_part_cap, part_bytes + row_bytes + (size_t)most * sizeof(double)));
     Part* parts = (Part*)c->list_part;
     Row* rows = (Row*)(c->list_part + part_bytes);
     double* row_loss = (double*)(c->list_part + part_bytes + row_bytes);
