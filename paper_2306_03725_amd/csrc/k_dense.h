@@ -114,6 +114,16 @@ struct StageKC {
             to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, g < left ? off : NOWHERE);
         }
     }
+    // the same of two matrices whose rows follow one another, `each` (a multiple of a load's rows) of them at a time
+    static __device__ __forceinline__ void direct_two(uint32_t lds, const char* const (&from)[2], int each, int rows, uint32_t pitch, int left) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int first = (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE, which = __builtin_amdgcn_readfirstlane(first >= each), g = group_of(t) * 16;
+            const i32x4 buffer = buffer_at(from[which]);
+            const uint32_t off = (uint32_t)min(row_of(t) - which * each, rows - 1) * pitch + (uint32_t)g;
+            to_lds(lds + (uint32_t)(first * KB), buffer, g < left ? off : NOWHERE);
+        }
+    }
     // the same through registers, for rows at any address: fetch, then (behind the step before) put
     // (before: bytes of K before the step)
     static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int rows, uint32_t pitch, int left, int before) {
@@ -126,6 +136,14 @@ struct StageKC {
                 const int g = group_of(t) * 16;
                 held[t] = sixteen(from + (size_t)min(row_of(t), rows - 1) * pitch + g, left - g, before + g);
             }
+        }
+    }
+    static __device__ __forceinline__ void fetch_two(i32x4 (&held)[LOADS], const char* const (&from)[2], int each, int rows, uint32_t pitch, int left, int before) {
+#pragma unroll
+        for (int t = 0; t < LOADS; ++t) {
+            const int which = (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE >= each, g = group_of(t) * 16;
+            const char* p = from[which] + (size_t)min(row_of(t) - which * each, rows - 1) * pitch + g;
+            held[t] = left >= KB ? *reinterpret_cast<const i32x4_any*>(p) : sixteen(p, left - g, before + g);
         }
     }
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {

@@ -36,29 +36,34 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
     constexpr int ROW = WD * (int)sizeof(TO), PITCH = ROW + 16, EACH = 16 / (int)sizeof(TO), GROUPS = ROW / 16;
     static_assert(N * 4 == WD, "four lanes share a row");
     const int l = (int)threadIdx.x & 63;
-    TO r[N];
+    if constexpr (N < EACH) {   // 8 bytes a lane: not worth the way
+        const int i = i0 + (l & 15), c = d0 + (l >> 4) * N;
+        if (i < b && c < d) put_many(to + (size_t)i * d + c, v, d - c);
+    } else {
+        TO r[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) r[j] = narrow<TO>(v[j]);
-    uint4 q[N / EACH > 0 ? N / EACH : 1];
-    __builtin_memcpy(q, r, sizeof(r));
+        for (int j = 0; j < N; ++j) r[j] = narrow<TO>(v[j]);
+        uint4 q[N / EACH > 0 ? N / EACH : 1];
+        __builtin_memcpy(q, r, sizeof(r));
 #pragma unroll
-    for (int u = 0; u < N / EACH; ++u) *reinterpret_cast<uint4*>(mine + (l & 15) * PITCH + (l >> 4) * (ROW / 4) + u * 16) = q[u];
+        for (int u = 0; u < N / EACH; ++u) *reinterpret_cast<uint4*>(mine + (l & 15) * PITCH + (l >> 4) * (ROW / 4) + u * 16) = q[u];
 #pragma unroll
-    for (int t = 0; t < 16 * GROUPS / 64; ++t) {
-        const int at = t * 64 + l, row = at / GROUPS, c = d0 + at % GROUPS * EACH, i = i0 + row;
-        const uint4 w = *reinterpret_cast<const uint4*>(mine + row * PITCH + at % GROUPS * 16);
-        if (i >= b || c >= d) continue;
-        TO* p = to + (size_t)i * d + c;
-        if (d - c >= EACH) {
-            typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
-            if (PAST_CACHES) __builtin_nontemporal_store(__builtin_bit_cast(Words, w), reinterpret_cast<Words*>(p));
-            else *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
-        } else {
-            TO one[EACH];
-            __builtin_memcpy(one, &w, 16);
+        for (int t = 0; t < 16 * GROUPS / 64; ++t) {
+            const int at = t * 64 + l, row = at / GROUPS, c = d0 + at % GROUPS * EACH, i = i0 + row;
+            const uint4 w = *reinterpret_cast<const uint4*>(mine + row * PITCH + at % GROUPS * 16);
+            if (i >= b || c >= d) continue;
+            TO* p = to + (size_t)i * d + c;
+            if (d - c >= EACH) {
+                typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+                if (PAST_CACHES) __builtin_nontemporal_store(__builtin_bit_cast(Words, w), reinterpret_cast<Words*>(p));
+                else *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
+            } else {
+                TO one[EACH];
+                __builtin_memcpy(one, &w, 16);
 #pragma unroll
-            for (int j = 0; j < EACH - 1; ++j)
-                if (j < d - c) p[j] = one[j];
+                for (int j = 0; j < EACH - 1; ++j)
+                    if (j < d - c) p[j] = one[j];
+            }
         }
     }
 }
@@ -71,9 +76,12 @@ k_dense_forward(Forward a) {
     constexpr int WAVES = WAVES_D * WAVES_B, KB = 64, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16;
     static_assert(DIRECT || STAGES == 2, "two sets of registers");
     using Acc = typename Core<T>::Acc;
-    using SV = StageKC<BD, KB, FD, WAVES>;   // (a lane's neighbours of all fragments are neighbours)
+    // V's rows, gate's before up's; a lane's neighbours of all fragments are neighbours.  TOGETHER: the rows of one matrix are too few for all wavefronts.
+    constexpr bool TOGETHER = BD < 16 * WAVES;
+    using SV = StageKC<MATS * BD, KB, FD, WAVES>;
+    using SQ = StageKC<TOGETHER ? MATS * BD : BD, KB, FD, WAVES>;
     using SE = StageKC<BB, KB, 1, WAVES>;
-    constexpr int STEP = MATS * SV::BYTES + SE::BYTES, LOADS = MATS * SV::LOADS + SE::LOADS;
+    constexpr int STEP = SV::BYTES + SE::BYTES, LOADS = SV::LOADS + SE::LOADS;
     extern __shared__ __align__(1024) char lds[];
     // Workgroups go to the chiplets in turn: the tiles of one piece of V, which share its rows, go to one of them, one after the other.
     const int turn = (int)blockIdx.x >> 3, td = turn / a.tiles_b * 8 + ((int)blockIdx.x & 7), tb = turn % a.tiles_b;
@@ -81,10 +89,9 @@ k_dense_forward(Forward a) {
     const int d0 = td * BD, b0 = tb * BB, wave = (int)threadIdx.x >> 6, wd = wave % WAVES_D * (BD / WAVES_D), wb = wave / WAVES_D * (BB / WAVES_B);
     const int rows_d = min(a.d - d0, BD), rows_b = min(a.b - b0, BB);
     const uint32_t pitch = (uint32_t)a.row_bytes;
-    const char* V[MATS];
+    const char *V[2], *e = (const char*)a.e + (size_t)b0 * pitch;
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) V[q] = (const char*)a.V[q] + (size_t)d0 * pitch;
-    const char* e = (const char*)a.e + (size_t)b0 * pitch;
+    for (int q = 0; q < 2; ++q) V[q] = (const char*)a.V[MATS == 1 ? 0 : q] + (size_t)d0 * pitch;
     Acc acc[MATS][FD][FB];
 #pragma unroll
     for (int q = 0; q < MATS; ++q)
@@ -103,17 +110,20 @@ k_dense_forward(Forward a) {
                 if (s >= steps) return;
                 const int at = s * KB, left = a.row_bytes - at;
                 const uint32_t to = lds_at(place(s));
+                const char* const from[2] = {V[0] + at, V[1] + at};
+                if constexpr (TOGETHER) SV::direct_two(to, from, BD, rows_d, pitch, left);
+                else
 #pragma unroll
-                for (int q = 0; q < MATS; ++q) SV::direct(to + q * SV::BYTES, V[q] + at, rows_d, pitch, left);
-                SE::direct(to + MATS * SV::BYTES, e + at, rows_b, pitch, left);
+                    for (int q = 0; q < MATS; ++q) SQ::direct(to + q * SQ::BYTES, from[q], rows_d, pitch, left);
+                SE::direct(to + SV::BYTES, e + at, rows_b, pitch, left);
             },
             [&](int s, i32x4 (&x)[FB]) {
 #pragma unroll
-                for (int f = 0; f < FB; ++f) x[f] = SE::frag(place(s) + MATS * SV::BYTES, lane_e, f);
+                for (int f = 0; f < FB; ++f) x[f] = SE::frag(place(s) + SV::BYTES, lane_e, f);
             },
             [&](int s, int g, i32x4 (&y)[Y]) {
 #pragma unroll
-                for (int f = 0; f < Y; ++f) y[f] = SV::frag(place(s) + (g * Y + f) / FD * SV::BYTES, lane_v, (g * Y + f) % FD);
+                for (int f = 0; f < Y; ++f) y[f] = SV::frag(place(s) + (g * Y + f) / FD * (BD * KB), lane_v, (g * Y + f) % FD);
             },
             [&](int g, const i32x4 (&x)[FB], const i32x4 (&y)[Y]) {
 #pragma unroll
@@ -125,17 +135,17 @@ k_dense_forward(Forward a) {
                     }
             });
     } else {
-        struct Held { i32x4 v[MATS][SV::LOADS], e[SE::LOADS]; };
+        struct Held { i32x4 v[TOGETHER ? 1 : MATS][SQ::LOADS], e[SE::LOADS]; };
         Held one, two;   // steps s + 1 and s + 2
         auto multiply = [&](const char* from) {
             i32x4 eb[FB];
 #pragma unroll
-            for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + MATS * SV::BYTES, lane_e, f);
+            for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + SV::BYTES, lane_e, f);
 #pragma unroll
             for (int q = 0; q < MATS; ++q)
 #pragma unroll
                 for (int f = 0; f < FD; ++f) {
-                    const i32x4 v = SV::frag(from + q * SV::BYTES, lane_v, f);
+                    const i32x4 v = SV::frag(from + q * (BD * KB), lane_v, f);
 #pragma unroll
                     for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
                 }
@@ -143,16 +153,19 @@ k_dense_forward(Forward a) {
         auto ask = [&](Held& h, int s) {
             if (s >= steps) return;
             const int at = s * KB, left = a.row_bytes - at;
+            const char* const from[2] = {V[0] + at, V[1] + at};
+            if constexpr (TOGETHER) SQ::fetch_two(h.v[0], from, BD, rows_d, pitch, left, at);
+            else
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) SV::fetch(h.v[q], V[q] + at, rows_d, pitch, left, at);
+                for (int q = 0; q < MATS; ++q) SQ::fetch(h.v[q], from[q], rows_d, pitch, left, at);
             SE::fetch(h.e, e + at, rows_b, pitch, left, at);
         };
         auto place = [&](const Held& h, int s) {
             if (s >= steps) return;
             char* to = lds + (s & 1) * STEP;
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) SV::put(to + q * SV::BYTES, h.v[q]);
-            SE::put(to + MATS * SV::BYTES, h.e);
+            for (int q = 0; q < (TOGETHER ? 1 : MATS); ++q) SQ::put(to + q * SQ::BYTES, h.v[q]);
+            SE::put(to + SV::BYTES, h.e);
         };
         ask(two, 0);
         ask(one, 1);
@@ -288,9 +301,13 @@ usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
     if (direct) {
         if (a.b > 128 && tiles(BD, 256) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, BD, 256, 2, 4, 4, true>(c, a, what);
         if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what);
+        if constexpr (MATS == 2)
+            if (tiles(64, 64) < c->num_cu) return launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, true>(c, a, what);
         return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what);
     }
     if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
+    if constexpr (MATS == 2)
+        if (tiles(64, 64) < c->num_cu) return launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, false>(c, a, what);
     return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
 }
 
