@@ -99,10 +99,12 @@ __device__ __forceinline__ int place_of(int row, int p) {
 }
 template <int ROWS, int KB, int SPREAD, int WAVES>
 struct StageKC {
-    static constexpr int AT_ONCE = 1024 / KB, LOADS = ROWS / AT_ONCE / WAVES;   // rows of a wavefront's load
-    static_assert(LOADS * AT_ONCE * WAVES == ROWS, "rows are dealt evenly");
+    // rows of a wavefront's load; where there are fewer loads than wavefronts, some ask for the same rows, so that all have asked for as many
+    static constexpr int AT_ONCE = 1024 / KB, LOADS = ROWS < AT_ONCE * WAVES ? 1 : ROWS / AT_ONCE / WAVES;
+    static_assert(ROWS % AT_ONCE == 0 && (ROWS < AT_ONCE * WAVES ? AT_ONCE * WAVES % ROWS == 0 : LOADS * AT_ONCE * WAVES == ROWS), "rows are dealt evenly");
     static constexpr int BYTES = ROWS * KB;
-    static __device__ __forceinline__ int row_of(int t) { return (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE + (int)(threadIdx.x & 63) / (KB / 16); }
+    static __device__ __forceinline__ int first_of(int t) { return (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE % ROWS; }
+    static __device__ __forceinline__ int row_of(int t) { return first_of(t) + (int)(threadIdx.x & 63) / (KB / 16); }
     static __device__ __forceinline__ int group_of(int t) { return place_of<KB, SPREAD>(row_of(t), (int)(threadIdx.x & 63) % (KB / 16)); }
     // from: row 0 of the tile at this step's first byte; rows: how many there are; left: bytes of K from here to the end (multiples of 16, as from's address)
     static __device__ __forceinline__ void direct(uint32_t lds, const char* from, int rows, uint32_t pitch, int left) {
@@ -111,14 +113,14 @@ struct StageKC {
         for (int t = 0; t < LOADS; ++t) {
             const int g = group_of(t) * 16;
             const uint32_t off = (uint32_t)min(row_of(t), rows - 1) * pitch + (uint32_t)g;
-            to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, g < left ? off : NOWHERE);
+            to_lds(lds + (uint32_t)(first_of(t) * KB), buffer, g < left ? off : NOWHERE);
         }
     }
     // the same of two matrices whose rows follow one another, `each` (a multiple of a load's rows) of them at a time
     static __device__ __forceinline__ void direct_two(uint32_t lds, const char* const (&from)[2], int each, int rows, uint32_t pitch, int left) {
 #pragma unroll
         for (int t = 0; t < LOADS; ++t) {
-            const int first = (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE, which = __builtin_amdgcn_readfirstlane(first >= each), g = group_of(t) * 16;
+            const int first = first_of(t), which = __builtin_amdgcn_readfirstlane(first >= each), g = group_of(t) * 16;
             const i32x4 buffer = buffer_at(from[which]);
             const uint32_t off = (uint32_t)min(row_of(t) - which * each, rows - 1) * pitch + (uint32_t)g;
             to_lds(lds + (uint32_t)(first * KB), buffer, g < left ? off : NOWHERE);
@@ -141,14 +143,14 @@ struct StageKC {
     static __device__ __forceinline__ void fetch_two(i32x4 (&held)[LOADS], const char* const (&from)[2], int each, int rows, uint32_t pitch, int left, int before) {
 #pragma unroll
         for (int t = 0; t < LOADS; ++t) {
-            const int which = (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE >= each, g = group_of(t) * 16;
+            const int which = first_of(t) >= each, g = group_of(t) * 16;
             const char* p = from[which] + (size_t)min(row_of(t) - which * each, rows - 1) * pitch + g;
             held[t] = left >= KB ? *reinterpret_cast<const i32x4_any*>(p) : sixteen(p, left - g, before + g);
         }
     }
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&held)[LOADS]) {
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + (t * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16) = held[t];
+        for (int t = 0; t < LOADS; ++t) *reinterpret_cast<i32x4*>(lds + first_of(t) * KB + (int)(threadIdx.x & 63) * 16) = held[t];
     }
     // Where this lane's 16 bytes of fragment 0 lie, row0 being the wavefront's first row of the tile (a multiple of 16 * SPREAD), and how far on those of
     // fragment f: the key of a row is that of its fragment's row.  KB = 64.

@@ -81,7 +81,7 @@ k_dense_forward(Forward a) {
     using SV = StageKC<MATS * BD, KB, FD, WAVES>;
     using SQ = StageKC<TOGETHER ? MATS * BD : BD, KB, FD, WAVES>;
     using SE = StageKC<BB, KB, 1, WAVES>;
-    constexpr int STEP = SV::BYTES + SE::BYTES, LOADS = SV::LOADS + SE::LOADS;
+    constexpr int STEP = SV::BYTES + SE::BYTES, LOADS = (TOGETHER ? 1 : MATS) * SQ::LOADS + SE::LOADS;
     extern __shared__ __align__(1024) char lds[];
     // Workgroups go to the chiplets in turn: the tiles of one piece of V, which share its rows, go to one of them, one after the other.
     const int turn = (int)blockIdx.x >> 3, td = turn / a.tiles_b * 8 + ((int)blockIdx.x & 7), tb = turn % a.tiles_b;
@@ -213,7 +213,8 @@ k_dense_forward(Forward a) {
     }
 }
 
-// At most 16 instances: the matrices go from memory into fragments, 16 rows to a workgroup whose wavefronts share K and join their sums through LDS.
+// At most 16 instances, few activations or rows at any address: the matrices go from memory into fragments, 16 rows to a workgroup whose wavefronts share K and join
+// their sums through LDS.  Bound by the rows' way from memory, 64 bytes of each to a load: 7 x 562 -> 37570 float32, 169 MB, 53 us.
 template <typename T, typename TO, int MATS, int ACT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_dense_few(Forward a) {
@@ -289,26 +290,30 @@ usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
     return usl_check_launch(c, what);
 }
 
+// Which tiles?  Large ones read V and e less often, but there have to be enough of them for the compute units, and instances to fill them.  us, gated, w = 768,
+// bfloat16 if not said otherwise:
+//   at most 16 instances   tiles of 64 x 16 where there is one for every compute unit, else the rows straight into fragments: 1 x -> 32768 19.2 and 21.6, 8 x -> 16384
+//                          9.8 and 11.6, 8 x -> 8192 7.2 and 7.1; 8 x -> 32768 float32 42.5 and 51.4 (tiles of 64 x 64: 57); 1 x 512 -> 65536 from 8 bits 10.0 and 10.5
+//   128 x 256              256 x -> 32768 37 where 128 x 128 take 46; 256 x -> 16384, half the compute units, 25 and 20
+//   128 x 128              128 x -> 32768 29.5 where 64 x 64 take 37; 64 x -> 32768 27 and 25 (float32 at 16 instances 103 and 58), 512 x -> 4096 18 and 14
+//   32 x 64                100 x 1000 -> 3000 9.8 where 64 x 64 take 12.1, 311 x 929 -> 1053 float32 34 and 48
 template <typename T, typename TO, int MATS, int ACT>
 usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
+    constexpr int FEW = MATS == 1 ? 128 : 64, MANY = MATS == 1 ? 256 : 128;
+    const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
+    auto enough = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b) >= c->num_cu; };
     if (a.b <= 16) {
+        if (direct && enough(FEW, 16)) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
         hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
-    constexpr int BD = MATS == 1 ? 256 : 128;
-    const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
-    auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
-    if (direct) {
-        if (a.b > 128 && tiles(BD, 256) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, BD, 256, 2, 4, 4, true>(c, a, what);
-        if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what);
-        if constexpr (MATS == 2)
-            if (tiles(64, 64) < c->num_cu) return launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, true>(c, a, what);
-        return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what);
-    }
-    if (tiles(128, 128) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
+    if (direct && a.b > 128 && enough(MANY, 256)) return launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, true>(c, a, what);
+    if (a.b > 64 && enough(128, 128))
+        return direct ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
     if constexpr (MATS == 2)
-        if (tiles(64, 64) < c->num_cu) return launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, false>(c, a, what);
-    return launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
+        if (!enough(64, 64))
+            return direct ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, false>(c, a, what);
+    return direct ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
 }
 
 }  // namespace dense

@@ -83,7 +83,8 @@ def test_forward_at_any_alignment(b, w, d, shift, storage):
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
-@pytest.mark.parametrize("b,w,d", [(130, 64, 16384), (300, 72, 16400), (257, 65, 20000)])
+@pytest.mark.parametrize("b,w,d", [(130, 64, 16384), (300, 72, 16400), (257, 65, 20000), (200, 136, 32770), (300, 40, 32768), (1, 64, 16384), (16, 200, 16390),
+                                   (7, 768, 32769), (15, 8, 16385), (65, 64, 32768), (64, 96, 16400)])
 def test_forward_of_large_tiles(b, w, d, storage):
     forward_case(b, w, d, storage, 0)
 
@@ -229,10 +230,10 @@ def test_gradients_against_differences(act):
     L.close()
 
 
-def test_another_stream_and_a_graph():
+@pytest.mark.parametrize("b,w,d", [(70, 136, 500), (300, 264, 16500), (5, 136, 16500)])
+def test_another_stream_and_a_graph(b, w, d):
     """On a stream of its own, captured and replayed with eager calls between: every replay gives the eager call's bits."""
     s = torch.cuda.Stream()
-    b, w, d = 70, 136, 500
     e, Vg, Vu = inputs(b, w, d, torch.bfloat16, seed=2)
     grad_x = torch.randn(b, d, device="cuda")
     L = usl().Layer(3, d, 1, b, "bf16", s.cuda_stream)
