@@ -405,14 +405,14 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         if (a.grad_V[0] || a.grad_V[1]) {
             // tiles of 256 columns where there is one for every compute unit
             if (a.w <= 128 || (int64_t)(a.wp / 256) * (2 * a.dp / 128) < c->num_cu) USL_TRY((grad_v<T, 128, 4>(c, a)));
-            else USL_TRY((grad_v<T, 256, 3>(c, a)));
+            else USL_TRY((grad_v<T, 256, 4>(c, a)));
         }
         if (!a.grad_e) continue;
         const Tiles t = cut(a, a.rows);
         const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
         if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, true>(c, a) : grad_e<T, 128, 128, 3, false>(c, a)));
         else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, true>(c, a) : grad_e<T, 256, 64, 3, false>(c, a)));
-        else USL_TRY((direct ? grad_e<T, 256, 128, 3, true>(c, a) : grad_e<T, 256, 128, 3, false>(c, a)));
+        else USL_TRY((direct ? grad_e<T, 256, 128, 4, true>(c, a) : grad_e<T, 256, 128, 3, false>(c, a)));
         const size_t n = (size_t)a.b * a.w;
         hipLaunchKernelGGL(k_gated_join, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, c->stream, a.sums, a.grad_e + (size_t)i0 * a.w, n, a.splits);
         USL_TRY(usl_check_launch(c, what));

@@ -28,7 +28,7 @@ def quantized(L, rows, shift=0):
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
-@pytest.mark.parametrize("n,w", [(1, 1), (3, 2), (5, 15), (4, 16), (7, 255), (2, 256), (3, 257), (6, 1000), (2, 4099), (1, 65536), (1000, 33)])
+@pytest.mark.parametrize("n,w", [(1, 1), (3, 2), (5, 15), (4, 16), (7, 255), (2, 256), (3, 257), (6, 1000), (2, 4099), (1, 65536), (1000, 33), (5, 2048), (5, 2049), (3, 511), (6, 513), (9, 8)])
 def test_codes(n, w, storage):
     gen = torch.Generator(device="cuda").manual_seed(n + w)
     rows = (torch.randn(n, w, device="cuda", generator=gen) * torch.exp(4 * torch.randn(n, 1, device="cuda", generator=gen))).to(TYPES[storage])
