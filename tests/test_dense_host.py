@@ -1,5 +1,6 @@
 """The calls in front of the layer and the losses against short lists refuse what they cannot take before anything is launched.  No GPU needed."""
 import os
+import re
 
 import pytest
 
@@ -90,25 +91,53 @@ def test_tensors_that_are_not_contiguous_are_refused(usl):
     L.close()
 
 
-def test_m0_belongs_to_the_tiles(tmp_path):
-    """The tiles' loads to LDS write M0 from inline assembly, which the compiler cannot be told: M0 must appear nowhere else in their kernels."""
-    import re
+@pytest.fixture(scope="module")
+def listings(tmp_path_factory):
+    """The compiler's listings of the kernels whose tiles are loaded to LDS by inline assembly."""
     import subprocess
 
     from paper_2306_03725_amd import build
-    for name in ("k_gated.hip", "k_gated_grad.hip"):
-        out = str(tmp_path / (name + ".s"))
+    lines = {}
+    for name in ("k_gated.hip", "k_gated_grad.hip", "k_int8.hip"):
+        out = str(tmp_path_factory.mktemp("listings") / (name + ".s"))
         subprocess.check_call([build._hipcc()] + build.FLAGS + ["--cuda-device-only", "-S", os.path.join(build.CSRC, name), "-o", out], stderr=subprocess.DEVNULL)
-        inside, own, other = False, 0, []
         with open(out) as fh:
-            for line in fh:
-                if "ASMSTART" in line:
-                    inside = True
-                elif "ASMEND" in line:
-                    inside = False
-                elif re.search(r"\bm0\b", line.split(";")[0]):
-                    if inside:
-                        own += 1
-                    else:
-                        other.append(line.strip())
+            lines[name] = fh.read().splitlines()
+    return lines
+
+
+def test_m0_belongs_to_the_tiles(listings):
+    """The tiles' loads to LDS write M0 from inline assembly, which the compiler cannot be told: M0 must appear nowhere else in their kernels."""
+    for name, lines in listings.items():
+        inside, own, other = False, 0, []
+        for line in lines:
+            if "ASMSTART" in line:
+                inside = True
+            elif "ASMEND" in line:
+                inside = False
+            elif re.search(r"\bm0\b", line.split(";")[0]):
+                if inside:
+                    own += 1
+                else:
+                    other.append(line.strip())
         assert own > 0 and not other, (name, other[:5])
+
+
+def test_no_read_of_a_step_crosses_a_barrier(listings):
+    """Behind a barrier the tiles' loads overwrite the step before it: a wavefront's reads from LDS have to be there when it comes to the barrier.  In the order of the
+    listing, which is that of the loops' bodies."""
+    barriers = 0
+    for name, lines in listings.items():
+        outstanding = False
+        for line in lines:
+            code = line.split(";")[0]
+            if re.match(r"_Z\w+:", code):
+                outstanding = False
+            if "ds_read" in code:
+                outstanding = True
+            if re.search(r"s_waitcnt.*lgkmcnt\(0\)", code):
+                outstanding = False
+            if "s_barrier" in code:
+                barriers += 1
+                assert not outstanding, (name, line)
+    assert barriers > 50
