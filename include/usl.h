@@ -316,7 +316,8 @@ usl_status usl_gated_block(usl_ctx* ctx, const void* e, const void* V_gate, cons
  *   grad_e = G_gate V_gate + G_up V_up [b][w],  grad_V_gate = G_gate^T e,  grad_V_up = G_up^T e [d][w]
  * e, V_gate, V_up as the forward call had them, gate and up as it left them.  grad_x and the results are float32, overwritten; each result may be
  * NULL, and none may be an input or another result.  Everything is computed in float32.  Where e, a matrix or G holds an infinity, the sums that it enters
- * are infinite or NaN.  Sums are taken in a fixed order: equal calls give equal bits.  Scratch is sized by w: a larger w than before reallocates and waits. */
+ * are infinite or NaN.  Sums are taken in a fixed order: equal calls give equal bits.  Scratch is sized for max_b and w; a call with a larger w than any before
+ * allocates (what it had is kept until usl_destroy, for graphs that were captured with it). */
 usl_status usl_gated_block_backward(usl_ctx* ctx, const float* grad_x, const void* e, const void* V_gate, const void* V_up, const void* gate,
                                     const void* up, int32_t w, int32_t act, float* grad_e, float* grad_V_gate, float* grad_V_up, int32_t b);
 
@@ -353,7 +354,7 @@ usl_status usl_distill_loss_grad(usl_ctx* ctx, const float* out, const int64_t* 
  *   logp[e] = log softmax(out[i])[act_lab[e]],  r = exp(logp - old_logp),  u = ref_logp - logp
  *   loss = scale * sum_e [ -min(r * advantage, clamp(r, 1 - clip_low, 1 + clip_high) * advantage) + beta * (exp(u) - u - 1) ]
  *   g = its gradient by out.  (Where both sides of the minimum are equal, that of the first.)
- * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0, all finite; ref_logp may be NULL if beta is 0.  logp: float32, one for each entry, a result (-infinity for an entry that does not
+ * 0 <= clip_low <= 1, clip_high >= 0, beta >= 0, all finite; ref_logp may be NULL if beta is 0.  old_logp and ref_logp of entries that count must be finite.  logp: float32, one for each entry, a result (-infinity for an entry that does not
  * count), or NULL; it must not be an input.  With g NULL this is also how old_logp and ref_logp are made. */
 usl_status usl_policy_loss_grad(usl_ctx* ctx, const float* out, const int64_t* act_off, const int32_t* act_lab, const float* old_logp,
                                 const float* ref_logp, const float* advantage, float clip_low, float clip_high, float beta, float scale,

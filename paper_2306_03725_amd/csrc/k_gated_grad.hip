@@ -384,7 +384,7 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
     };
     // pieces' sums: no more tiles than compute units, of 128 x 256 at most, or one piece of everything
     const size_t by_tiles = (size_t)c->num_cu * 128 * 256, sums_most = by_tiles > most * a.w ? by_tiles : most * (size_t)a.w;
-    USL_TRY(usl_reserve(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, most * row + sums_most * 4));
+    USL_TRY(usl_reserve_kept(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, most * row + sums_most * 4));
     a.G = c->gated_scratch;
     const char *e = (const char*)a.e, *gate = (const char*)a.gate, *up = (const char*)a.up;
     const float* grad_x = a.grad_x;

@@ -147,7 +147,7 @@ struct Entry {
         z = score_of(a, row, a.lab[e], counts);
         if (TEACHER) {
             value = a.logit[e];
-            counts = counts && !(value * a.inv_t == -INFINITY);
+            counts = counts && !(value == -INFINITY);
         }
     }
 };

@@ -42,6 +42,7 @@ extern "C" usl_status usl_destroy(usl_ctx* c) {
             for (void* p : lists)
                 if (p) (void)hipFree(p);
         }
+        for (int n = 0; n < c->outgrown_n; ++n) (void)hipFree(c->outgrown[n]);
         if (c->hint_host) (void)hipHostFree(c->hint_host);
     }
     free(c);
@@ -94,6 +95,20 @@ usl_status usl_reserve(usl_ctx* c, void** buf, size_t* cap, size_t bytes) {
         *buf = nullptr;
         USL_FAIL(c, USL_ENOMEM, "hipMalloc of %zu bytes failed: %s", bytes, hipGetErrorString(e));
     }
+    *cap = bytes;
+    return USL_OK;
+}
+
+usl_status usl_reserve_kept(usl_ctx* c, void** buf, size_t* cap, size_t bytes) {
+    if (*buf && *cap >= bytes) return USL_OK;
+    const int room = (int)(sizeof(c->outgrown) / sizeof(c->outgrown[0]));
+    if (*buf && c->outgrown_n == room) USL_FAIL(c, USL_ENOMEM, "scratch has grown %d times", room);
+    if (*buf && bytes < *cap + *cap / 2) bytes = *cap + *cap / 2;   // 32 times are enough for any need
+    void* grown = nullptr;
+    hipError_t e = hipMalloc(&grown, bytes);
+    if (e != hipSuccess) USL_FAIL(c, USL_ENOMEM, "hipMalloc of %zu bytes failed: %s", bytes, hipGetErrorString(e));
+    if (*buf) c->outgrown[c->outgrown_n++] = *buf;
+    *buf = grown;
     *cap = bytes;
     return USL_OK;
 }

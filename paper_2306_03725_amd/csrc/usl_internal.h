@@ -68,6 +68,7 @@ struct usl_ctx {
     bool topk_done_clear;          // it has been cleared
     float* norm_part;         size_t norm_part_cap;  // [parts of the batch][2][d] sums of the layer norm's weight and bias gradients
     char* gated_scratch;      size_t gated_scratch_cap;  // the gated block's backward pass: gradients by its projections, e, sums of grad_e (k_gated_grad.hip)
+    void* outgrown[32];       int outgrown_n;            // scratch that was too small for a later call: kept, because captured graphs may still use it (usl_reserve_kept)
     char* list_part;          size_t list_part_cap;  // losses against short lists: sums of segments, rows, rows' losses (k_list_loss.hip)
     float* gw_part;           size_t gw_part_cap;   // [groups][m*k] partial weight gradients of a split batch
     int gw_parts_most;             // groups that it has room for (0: not known yet)
@@ -130,6 +131,7 @@ struct usl_ctx {
 // Makes the device current on first use and reads its compute-unit count.
 usl_status usl_prepare_device(usl_ctx* ctx);
 // Grows *buf to at least `bytes` (old contents are dropped).
+usl_status usl_reserve_kept(usl_ctx* ctx, void** buf, size_t* cap, size_t bytes);   // the same for scratch whose need a call's arguments set: the old one lives on
 usl_status usl_reserve(usl_ctx* ctx, void** buf, size_t* cap, size_t bytes);
 // The per-block loss sums of every loss kernel, for max_b instances: no later call has to grow them (growing frees and
 // allocates, which waits for the stream).  usl_forward_blocks: workgroups that forward may have when it sums the loss.

@@ -265,3 +265,40 @@ def test_another_stream_and_a_graph(b, w, d):
         assert all(torch.equal(a, c) for a, c in zip(eager, mine)), turn
     del g
     L.close()
+
+
+def test_a_graph_survives_a_call_that_needs_more_scratch():
+    """Captured with a narrow e, then an eager call with a wide one, which needs more scratch than there is: the graph's is still its own."""
+    s = torch.cuda.Stream()
+    b, d = 40, 300
+    L = usl().Layer(3, d, 1, b, "bf16", s.cuda_stream)
+
+    def make(w):
+        e, Vg, Vu = inputs(b, w, d, torch.bfloat16, seed=w)
+        gate, up = ((e.float() @ V.float().t()).bfloat16() for V in (Vg, Vu))
+        o = [torch.full((b, w), float("nan"), device="cuda"), torch.full((d, w), float("nan"), device="cuda"), torch.full((d, w), float("nan"), device="cuda")]
+        return (torch.randn(b, d, device="cuda"), e, Vg, Vu, gate, up, w, 0), o
+
+    (narrow, out), (wide, out_wide) = make(64), make(40000)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        L.gated_block_backward(*narrow, *out, b)
+    s.synchronize()
+    want = [o.clone() for o in out]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        L.gated_block_backward(*narrow, *out, b)
+    for _ in range(3):
+        with torch.cuda.stream(s):
+            L.gated_block_backward(*wide, *out_wide, b)
+            for o in out:
+                o.fill_(float("nan"))
+            g.replay()
+        s.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(out, want))
+    with torch.cuda.stream(s):
+        L.gated_block_backward(*narrow, *out, b)
+    s.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(out, want))
+    del g
+    L.close()

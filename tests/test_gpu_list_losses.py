@@ -104,6 +104,25 @@ def test_distill_of_hard_lists(wide):
         assert bool((g[[2, 4, 5, 6]] == 0).all()) and bool((g[1] != 0).any())
 
 
+def test_temperatures_far_from_one():
+    """Logits and scores whose quotients by T leave float32's range, and those that vanish in it: the entries count all the same."""
+    off, lab, gen = lists(2, 6000, [3, 2], 3)
+    out = torch.randn(2, 6000, generator=gen)
+    L = layer(6000, 2)
+    for T, size in ((1e-30, 1e12), (1e30, 1.0)):
+        logit = torch.randn(5, generator=gen) * size
+        g, loss = torch.empty(2, 6000, device="cuda"), torch.empty(1, device="cuda")
+        L.distill_loss_grad(out.cuda(), off.cuda(), lab.cuda(), logit.cuda(), T, 1.0 / T if T > 1 else 1e30, g, loss, 2)
+        # scale * T = 1: g = q - p, q one-hot or flat, p one-hot or flat
+        want = torch.zeros(2, 6000)
+        for i in range(2):
+            want[i] = torch.softmax(out[i].double() / T, 0).float()
+            e = slice(int(off[i]), int(off[i + 1]))
+            want[i].index_add_(0, lab[e].long(), -torch.softmax(logit[e].double() / T, 0).float())
+        assert torch.allclose(g.cpu(), want, rtol=1e-5, atol=1e-6), (T, float((g.cpu() - want).abs().max()))
+    L.close()
+
+
 def policy_case(out, off, lab, old, ref, adv, low, high, beta, scale, in_place=False, L=None):
     b, m = out.shape
     own = L or layer(m, b)
