@@ -1,5 +1,7 @@
 // Kernels of one or two projections of the rows of e, with what follows them in the epilogue (k_gated.hip, k_int8.hip).
 #pragma once
+#include <math.h>
+
 #include "k_dense.h"
 
 namespace dense {
@@ -213,15 +215,14 @@ k_dense_forward(Forward a) {
     }
 }
 
-// At most 16 instances, few activations or rows at any address: the matrices go from memory into fragments, 16 rows to a workgroup whose wavefronts share K and join
-// their sums through LDS.  Bound by the rows' way from memory, 64 bytes of each to a load: 7 x 562 -> 37570 float32, 169 MB, 53 us.
+// Few results: the matrices go from memory into fragments, 16 rows and 16 instances to a workgroup whose wavefronts share K and join their sums through LDS.  Bound by the rows' way from memory, 64 bytes of each to a load: 7 x 562 -> 37570 float32, 169 MB, 53 us.
 template <typename T, typename TO, int MATS, int ACT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_dense_few(Forward a) {
     using Acc = typename Core<T>::Acc;
     __shared__ Acc sums[WAVES][MATS][64];
-    const int l = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, d0 = (int)blockIdx.x * 16;
-    const size_t row_v = (size_t)min(d0 + (l & 15), a.d - 1) * a.row_bytes, row_e = (size_t)min(l & 15, a.b - 1) * a.row_bytes;
+    const int l = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, d0 = (int)blockIdx.x * 16, i = (int)blockIdx.y * 16 + (l & 15);
+    const size_t row_v = (size_t)min(d0 + (l & 15), a.d - 1) * a.row_bytes, row_e = (size_t)min(i, a.b - 1) * a.row_bytes;
     const char* e = (const char*)a.e + row_e + (l >> 4) * 16;
     const char* V[MATS];
 #pragma unroll
@@ -252,10 +253,10 @@ k_dense_few(Forward a) {
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) acc[q] += sums[v][q][l];
     const int at = d0 + (l >> 4) * 4;
-    if ((l & 15) < a.b && at < a.d) {
+    if (i < a.b && at < a.d) {
         Scales<T, MATS, 4> scales;
         scales.load(a, at);
-        const float e_scale = sizeof(T) == 1 ? a.e_scale[l & 15] : 1.f;
+        const float e_scale = sizeof(T) == 1 ? a.e_scale[i] : 1.f;
         float v[MATS][4];
 #pragma unroll
         for (int q = 0; q < MATS; ++q)
@@ -264,7 +265,7 @@ k_dense_few(Forward a) {
                 v[q][j] = (float)acc[q][j];
                 if (sizeof(T) == 1) v[q][j] *= e_scale * scales.v[q][j];
             }
-        const size_t to = (size_t)(l & 15) * a.d + at;
+        const size_t to = (size_t)i * a.d + at;
         if (MATS == 1) {
             put_many((TO*)a.x + to, v[0], a.d - at);
             return;
@@ -290,28 +291,36 @@ usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
     return usl_check_launch(c, what);
 }
 
-// Which tiles?  Large ones read V and e less often, but there have to be enough of them for the compute units, and instances to fill them.  us, gated, w = 768,
-// bfloat16 if not said otherwise:
-//   at most 16 instances   tiles of 64 x 16 where there is one for every compute unit, else the rows straight into fragments: 1 x -> 32768 19.2 and 21.6, 8 x -> 16384
-//                          9.8 and 11.6, 8 x -> 8192 7.2 and 7.1; 8 x -> 32768 float32 42.5 and 51.4 (tiles of 64 x 64: 57); 1 x 512 -> 65536 from 8 bits 10.0 and 10.5
-//   128 x 256              256 x -> 32768 37 where 128 x 128 take 46; 256 x -> 16384, half the compute units, 25 and 20
-//   128 x 128              128 x -> 32768 29.5 where 64 x 64 take 37; 64 x -> 32768 27 and 25 (float32 at 16 instances 103 and 58), 512 x -> 4096 18 and 14
-//   32 x 64                100 x 1000 -> 3000 9.8 where 64 x 64 take 12.1, 311 x 929 -> 1053 float32 34 and 48
+// Which tiles?  A compute unit's time is that of the tiles that fall to it, whole ones of them, each as long as its area over its rate: large ones read fragments less often
+// (in float32 the matrix cores are so slow that it does not matter), small ones leave less undone at the edges and fall to the compute units more evenly.  Rates from
+// 512 x 768 -> 32768 (bfloat16 128 x 256 67 us, 128 x 128 83, 64 x 64 114, 32 x 64 160).  us, gated, w = 768, bfloat16 if not said otherwise, by what the rule takes and by others:
+//   256 x -> 32768  128 x 256 37, 128 x 128 46        256 x -> 16384  128 x 128 20, 128 x 256 25, 64 x 64 25
+//   128 x -> 32768  128 x 128 29.5, 64 x 64 37        64 x -> 32768   64 x 64 25, 128 x 128 27
+//   512 x -> 4096   64 x 64 14, 128 x 128 18          100 x 1000 -> 3000  32 x 64 9.8, 64 x 64 12.1
+//   float32: 169 x 256 -> 16512  64 x 64 40, 128 x 128 72;  1000 x 500 -> 20000  348 and 406;  512 x 768 -> 32768  128 x 256 398, 64 x 64 406
+// At most 16 instances: tiles of 64 x 16 where there is one for every compute unit: 1 x -> 32768 19.2, rows straight into fragments 21.6; 8 x -> 16384 9.8 and 11.6; 8 x -> 8192
+// 7.2 and 7.1; 8 x -> 32768 float32 42.5 and 51.4; 1 x 512 -> 65536 from 8 bits 10.0 and 10.5.
+// Rows straight into fragments otherwise, and for up to two fragments to a compute unit, whose wavefronts then share K: 48 x 1792 -> 64 6.9, 32 x 64 14.1; 58 x 1083 -> 1675
+// float32 17 and 39; 100 x 1000 -> 1000 8.9 and 9.7; not 200 x 512 -> 1024 (832 fragments) 7.6 and 6.3.
 template <typename T, typename TO, int MATS, int ACT>
 usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
     constexpr int FEW = MATS == 1 ? 128 : 64, MANY = MATS == 1 ? 256 : 128;
+    constexpr bool SLOW = sizeof(T) == 4;
     const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
-    auto enough = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b) >= c->num_cu; };
-    if (a.b <= 16) {
-        if (direct && enough(FEW, 16)) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
-        hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16)), dim3(256), 0, c->stream, a);
+    auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
+    if (direct && a.b <= 16 && tiles(FEW, 16) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
+    if (a.b <= 16 || tiles(16, 16) <= 2 * c->num_cu) {
+        hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16), (unsigned)((a.b + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
-    if (direct && a.b > 128 && enough(MANY, 256)) return launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, true>(c, a, what);
-    if (a.b > 64 && enough(128, 128))
+    auto cost = [&](int d, int b, double rate) { return (double)((tiles(d, b) + c->num_cu - 1) / c->num_cu) * d * b / rate; };
+    const double by_many = direct ? cost(MANY, 256, 1.0) : INFINITY, by_128 = cost(128, 128, SLOW ? 1.0 : 0.8), by_64 = cost(64, 64, SLOW ? 0.97 : 0.59),
+                 by_32 = MATS == 2 ? cost(32, 64, SLOW ? 0.9 : 0.42) : INFINITY;
+    if (by_many <= by_128 && by_many <= by_64 && by_many <= by_32) return launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, true>(c, a, what);
+    if (by_128 <= by_64 && by_128 <= by_32)
         return direct ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
     if constexpr (MATS == 2)
-        if (!enough(64, 64))
+        if (by_32 < by_64)
             return direct ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, false>(c, a, what);
     return direct ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
 }

@@ -84,7 +84,8 @@ def test_forward_at_any_alignment(b, w, d, shift, storage):
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("b,w,d", [(130, 64, 16384), (300, 72, 16400), (257, 65, 20000), (200, 136, 32770), (300, 40, 32768), (1, 64, 16384), (16, 200, 16390),
-                                   (7, 768, 32769), (15, 8, 16385), (65, 64, 32768), (64, 96, 16400)])
+                                   (7, 768, 32769), (15, 8, 16385), (65, 64, 32768), (64, 96, 16400), (257, 64, 33000), (169, 72, 16512),
+                                   (700, 40, 9000), (129, 33, 12000), (47, 900, 64), (250, 130, 400)])
 def test_forward_of_large_tiles(b, w, d, storage):
     forward_case(b, w, d, storage, 0)
 
