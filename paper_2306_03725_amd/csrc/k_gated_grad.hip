@@ -130,21 +130,21 @@ __device__ __forceinline__ bool tile_of(int inner, int outer, int& in, int& out)
 }
 unsigned tiles_grid(int inner, int outer) { return (unsigned)((inner * outer + 7) / 8 * 8); }
 
-// grad_V: [w] along m, [2][d] along n, the instances along K.  Tiles of MT x 128, a wavefront 64 x 64 of it.  The parts of G meet the same fragments of e, so
+// grad_V: [w] along m, [2][d] along n, the instances along K.  Tiles of MT x NT, a wavefront F x F fragments of it.  The parts of G meet the same fragments of e, so
 // what has to come from the caches for a product on the matrix cores falls with MT.
-template <typename T, int MT, int STAGES>
-__global__ void __launch_bounds__(2 * MT, 2)
+template <typename T, int MT, int NT, int F, int STAGES>
+__global__ void __launch_bounds__(MT * NT / (4 * F * F), 2)
 k_gated_grad_v(Grad a) {
-    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 32;
+    constexpr int P = PARTS<T>, WM = F * 16, WAVES = MT / WM * (NT / WM);
     using SE = StageKO<T, MT, WAVES>;
-    using SG = StageKO<T, 128, WAVES>;
+    using SG = StageKO<T, NT, WAVES>;
     constexpr int STEP = SE::BYTES + P * SG::BYTES, LOADS = SE::LOADS + P * SG::LOADS;
     extern __shared__ __align__(1024) char lds[];
     int tm, tn;
-    if (!tile_of(a.tiles_m, 2 * a.dp / 128, tm, tn)) return;
-    const int m0 = tm * MT, n0 = tn * 128, wave = (int)threadIdx.x >> 6, wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    if (!tile_of(a.tiles_m, 2 * a.dp / NT, tm, tn)) return;
+    const int m0 = tm * MT, n0 = tn * NT, wave = (int)threadIdx.x >> 6, wm = wave / (NT / WM) * WM, wn = wave % (NT / WM) * WM;
     const size_t pitch_e = (size_t)a.wp * sizeof(T), pitch_g = 128 * sizeof(T), next_part = (size_t)a.rows * 2 * a.dp * sizeof(T);
-    const char *E = a.E + (size_t)m0 * sizeof(T), *G = a.G + (size_t)tn * a.rows * pitch_g;
+    const char *E = a.E + (size_t)m0 * sizeof(T), *G = a.G + (size_t)(n0 >> 7) * a.rows * pitch_g + (size_t)(n0 & 127) * sizeof(T);
     f32x4 acc[F][F];
 #pragma unroll
     for (int f = 0; f < F; ++f)
@@ -201,12 +201,12 @@ k_gated_grad_v(Grad a) {
     }
 }
 
-// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  Tiles of MT x NT, a wavefront 64 x 64 of it.  DIRECT: V's rows and bases are
+// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  Tiles of MT x NT, a wavefront 64 x 16 * FN of it.  DIRECT: V's rows and bases are
 // multiples of 16 bytes; else V comes through registers, asked for two steps ahead and put into LDS one step ahead.
-template <typename T, int MT, int NT, int STAGES, bool DIRECT>
-__global__ void __launch_bounds__(MT * NT / 64, 2)
+template <typename T, int MT, int NT, int FN, int STAGES, bool DIRECT>
+__global__ void __launch_bounds__(MT * NT / (16 * FN), 2)
 k_gated_grad_e(Grad a) {
-    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / 64);
+    constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / (FN * 16));
     using SV = StageKO<T, MT, WAVES>;
     using SG = StageKC<NT, 64, 1, WAVES>;
     constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (DIRECT ? SV::LOADS : 0) + P * SG::LOADS;
@@ -214,14 +214,14 @@ k_gated_grad_e(Grad a) {
     extern __shared__ __align__(1024) char lds[];
     int tile, piece;
     if (!tile_of(a.tiles_m * a.tiles_n, a.splits, tile, piece)) return;
-    const int m0 = tile % a.tiles_m * MT, n0 = tile / a.tiles_m * NT, wave = (int)threadIdx.x >> 6, wm = wave % (MT / 64) * 64, wn = wave / (MT / 64) * 64;
+    const int m0 = tile % a.tiles_m * MT, n0 = tile / a.tiles_m * NT, wave = (int)threadIdx.x >> 6, wm = wave % (MT / 64) * 64, wn = wave / (MT / 64) * (FN * 16);
     const size_t pitch_v = (size_t)a.w * sizeof(T), pitch_g = 128 * sizeof(T), next_part = (size_t)a.rows * 2 * a.dp * sizeof(T);
     const int rows = a.rows - n0;   // (those behind the last instance hold zeros)
-    f32x4 acc[F][F];
+    f32x4 acc[F][FN];
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
-        for (int h = 0; h < F; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
+        for (int h = 0; h < FN; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
     const int first = piece * a.steps_each, steps = min(a.steps_each, 2 * a.dp / SV::DEPTH - first);
     int lane_v[F];
 #pragma unroll
@@ -244,20 +244,20 @@ k_gated_grad_e(Grad a) {
         if constexpr (DIRECT) SV::direct(lds_at(place(s)), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
         else SV::fetch(h->v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
     };
-    constexpr int GROUPS = P > 1 ? P : 2, Y = P * F / GROUPS;
+    constexpr int GROUPS = P > 1 ? P : 2, Y = P * FN / GROUPS;
     auto first_of = [&](int s, i32x4 (&x)[F]) {
 #pragma unroll
         for (int f = 0; f < F; ++f) x[f] = SV::frag(place(s), lane_v[f]);
     };
     auto group_of = [&](int s, int g, i32x4 (&y)[Y]) {
 #pragma unroll
-        for (int h = 0; h < Y; ++h) y[h] = SG::frag(place(s) + SV::BYTES + (P - 1 - (g * Y + h) / F) * SG::BYTES, lane_g, (g * Y + h) % F);
+        for (int h = 0; h < Y; ++h) y[h] = SG::frag(place(s) + SV::BYTES + (P - 1 - (g * Y + h) / FN) * SG::BYTES, lane_g, (g * Y + h) % FN);
     };
     auto multiply = [&](int g, const i32x4 (&x)[F], const i32x4 (&y)[Y]) {
 #pragma unroll
         for (int h = 0; h < Y; ++h)
 #pragma unroll
-            for (int f = 0; f < F; ++f) acc[f][(g * Y + h) % F] = Core<T>::mul(x[f], y[h], acc[f][(g * Y + h) % F]);
+            for (int f = 0; f < F; ++f) acc[f][(g * Y + h) % FN] = Core<T>::mul(x[f], y[h], acc[f][(g * Y + h) % FN]);
     };
     if constexpr (DIRECT) {
         walk<F, GROUPS, Y, STAGES>(
@@ -297,7 +297,7 @@ k_gated_grad_e(Grad a) {
     const int l = (int)threadIdx.x & 63;
     float* sums = a.sums + (size_t)piece * a.b * a.w;
 #pragma unroll
-    for (int h = 0; h < F; ++h) {
+    for (int h = 0; h < FN; ++h) {
         const int i = n0 + wn + h * 16 + (l & 15);
         if (i >= a.b) continue;
 #pragma unroll
@@ -332,31 +332,43 @@ usl_status lds_for(usl_ctx* c, F* kernel, int bytes) {
     return USL_OK;
 }
 
-template <typename T, int MT, int STAGES>
+template <typename T, int MT, int NT, int F, int STAGES>
 usl_status grad_v(usl_ctx* c, Grad a) {
-    constexpr int BYTES = STAGES * (MT + PARTS<T> * 128) * 64;
-    USL_TRY(lds_for(c, k_gated_grad_v<T, MT, STAGES>, BYTES));
+    constexpr int BYTES = STAGES * (MT + PARTS<T> * NT) * 64;
+    USL_TRY(lds_for(c, k_gated_grad_v<T, MT, NT, F, STAGES>, BYTES));
     a.tiles_m = (a.w + MT - 1) / MT;
-    hipLaunchKernelGGL((k_gated_grad_v<T, MT, STAGES>), dim3(tiles_grid(a.tiles_m, 2 * a.dp / 128)), dim3(2 * MT), BYTES, c->stream, a);
+    hipLaunchKernelGGL((k_gated_grad_v<T, MT, NT, F, STAGES>), dim3(tiles_grid(a.tiles_m, 2 * a.dp / NT)), dim3(MT * NT / (4 * F * F)), BYTES, c->stream, a);
     return usl_check_launch(c, "gated_block_backward");
 }
 
-template <typename T, int MT, int NT, int STAGES, bool DIRECT>
+template <typename T, int MT, int NT, int FN, int STAGES, bool DIRECT>
 usl_status grad_e(usl_ctx* c, Grad a) {
     constexpr int BYTES = STAGES * (MT + PARTS<T> * NT) * 64;
-    USL_TRY(lds_for(c, k_gated_grad_e<T, MT, NT, STAGES, DIRECT>, BYTES));
-    hipLaunchKernelGGL((k_gated_grad_e<T, MT, NT, STAGES, DIRECT>), dim3(tiles_grid(a.tiles_m * a.tiles_n, a.splits)), dim3(MT * NT / 64), BYTES, c->stream, a);
+    USL_TRY(lds_for(c, k_gated_grad_e<T, MT, NT, FN, STAGES, DIRECT>, BYTES));
+    hipLaunchKernelGGL((k_gated_grad_e<T, MT, NT, FN, STAGES, DIRECT>), dim3(tiles_grid(a.tiles_m * a.tiles_n, a.splits)), dim3(MT * NT / (16 * FN)), BYTES, c->stream, a);
     return usl_check_launch(c, "gated_block_backward");
 }
 
-// Tiles of grad_e.  Instances 64 at a time where there are no more; 256 columns of w where every compute unit then has at least 16 steps to go, else 128, which share
-// the work among twice the workgroups and leave half the sums.  (Backward of 300 x 200 -> 1000 float32 with this rule and that of grad_v 41 us, with 256 columns 67;
-// 900 x 1260 -> 148 bfloat16 51 and 63; 100 x 509 -> 4099 float32 55.6 and 57.7.)
+// Tiles of grad_e.  Instances 32 or 64 at a time where there are no more; 256 columns of w where every compute unit then has at least 16 steps to go, else 128, which share
+// the work among twice the workgroups and leave half the sums.  (Backward of 300 x 200 -> 1000 float32, 25 us, 7 more with 256 columns; of
+// 1 x 130 -> 45688 float32 with 32 instances at a time 117 us, with 64 at a time 127; 32 x 512 -> 16384 55 and 57.)
 struct Tiles { int m, n; };
 Tiles tiles_of(const usl_ctx* c, int w, int rows, int k_steps) {
-    const int n = rows <= 64 ? 64 : 128;
+    const int n = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     const bool wide = w > 128 && (int64_t)((w + 255) / 256) * ((rows + n - 1) / n) * (k_steps / 16) >= c->num_cu;
     return wide ? Tiles{256, n} : Tiles{128, 128};
+}
+
+// Tiles of grad_V, 64 x 64 or 256 x 128 of the values of grad_V.  The tall ones take half of what the small ones do from the caches for a product on the matrix
+// cores.  With float32 storage, whose products take four instructions each, that is never the bound and the small tiles share the work better.  With bfloat16 a compute unit does a
+// value of a small tile at 0.55 of the rate, and the choice is by what falls to the unit that has the most.  (Whole backward passes, small tiles and tall ones:
+// float32 512 x 768 -> 8192 242 and 278 us, 64 x 256 -> 131072 226 and 244, 300 x 200 -> 1000 25 and 60; bfloat16 512 x 768 -> 32768 440 and 373,
+// 512 x 1024 -> 4096 88 and 81, 680 x 256 -> 17920 156 and 157, 256 x 512 -> 4096 35 and 38, 779 x 1302 -> 357 39 and 59.)
+template <typename T>
+bool tall_v(const usl_ctx* c, int w, int dp) {
+    if (sizeof(T) == 4 || w <= 128) return false;
+    auto most = [&](int m, int n) { return ((int64_t)((w + m - 1) / m) * (2 * dp / n) + c->num_cu - 1) / c->num_cu * m * n; };
+    return most(256, 128) * 0.55 <= most(64, 64);
 }
 
 template <typename T>
@@ -403,16 +415,16 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         else hipLaunchKernelGGL((k_gated_slopes<T, 1>), slopes, dim3(PREP_NT), 0, c->stream, a);
         USL_TRY(usl_check_launch(c, what));
         if (a.grad_V[0] || a.grad_V[1]) {
-            // tiles of 256 columns where there is one for every compute unit
-            if (a.w <= 128 || (int64_t)(a.wp / 256) * (2 * a.dp / 128) < c->num_cu) USL_TRY((grad_v<T, 128, 4>(c, a)));
-            else USL_TRY((grad_v<T, 256, 4>(c, a)));
+            if (tall_v<T>(c, a.w, a.dp)) USL_TRY((grad_v<T, 256, 128, 4, 4>(c, a)));
+            else USL_TRY((grad_v<T, 64, 64, 2, 4>(c, a)));
         }
         if (!a.grad_e) continue;
         const Tiles t = cut(a, a.rows);
         const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
-        if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, true>(c, a) : grad_e<T, 128, 128, 3, false>(c, a)));
-        else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, true>(c, a) : grad_e<T, 256, 64, 3, false>(c, a)));
-        else USL_TRY((direct ? grad_e<T, 256, 128, 4, true>(c, a) : grad_e<T, 256, 128, 3, false>(c, a)));
+        if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, 4, true>(c, a) : grad_e<T, 128, 128, 4, 3, false>(c, a)));
+        else if (t.n == 32) USL_TRY((direct ? grad_e<T, 256, 32, 2, 4, true>(c, a) : grad_e<T, 256, 32, 2, 3, false>(c, a)));
+        else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, 4, true>(c, a) : grad_e<T, 256, 64, 4, 3, false>(c, a)));
+        else USL_TRY((direct ? grad_e<T, 256, 128, 4, 4, true>(c, a) : grad_e<T, 256, 128, 4, 3, false>(c, a)));
         const size_t n = (size_t)a.b * a.w;
         hipLaunchKernelGGL(k_gated_join, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, c->stream, a.sums, a.grad_e + (size_t)i0 * a.w, n, a.splits);
         USL_TRY(usl_check_launch(c, what));

@@ -160,6 +160,12 @@ def test_backward(b, w, d, storage):
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("b,w,d", [(5, 264, 33000), (32, 301, 33000), (33, 264, 33000), (64, 299, 33001), (150, 500, 8100), (130, 384, 16400), (17, 513, 8192)])
+def test_backward_of_large_tiles(b, w, d, storage):
+    backward_case(b, w, d, storage, b % 2)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("b,w,d,shift", [(5, 64, 64, 1), (70, 64, 130, 2), (70, 48, 64, 4), (40, 71, 68, 1), (40, 130, 66, 8)])
 def test_backward_at_any_alignment(b, w, d, shift, storage):
     backward_case(b, w, d, storage, 0, shift=shift)
