@@ -349,12 +349,15 @@ usl_status grad_e(usl_ctx* c, Grad a) {
     return usl_check_launch(c, "gated_block_backward");
 }
 
-// Tiles of grad_e.  Instances 32 or 64 at a time where there are no more; 256 columns of w where every compute unit then has at least 16 steps to go, else 128, which share
-// the work among twice the workgroups and leave half the sums.  (Backward of 300 x 200 -> 1000 float32, 25 us, 7 more with 256 columns; of
-// 1 x 130 -> 45688 float32 with 32 instances at a time 117 us, with 64 at a time 127; 32 x 512 -> 16384 55 and 57.)
+// Tiles of grad_e.  Instances 32 or 64 at a time where there are no more, and 64 where V comes straight into LDS and they leave out an eighth of what 128 at a time
+// would multiply; 256 columns of w where every compute unit then has at least 16 steps to go, else 128, which share the work among twice the workgroups and leave
+// half the sums.  (Backward of 300 x 200 -> 1000 float32, 25 us, 7 more with 256 columns; of 1 x 130 -> 45688 float32 with 32 instances at a time 117 us, with 64 at a time 127;
+// with 64 and 128 at a time: 155 x 256 -> 55424 float32 221 and 244, bfloat16 140 and 145, 300 x 384 -> 16384 float32 193 and 204, 512 x 768 -> 16384 482 and 457,
+// 200 x 301 -> 30001, V through registers, 458 and 288.)
 struct Tiles { int m, n; };
-Tiles tiles_of(const usl_ctx* c, int w, int rows, int k_steps) {
-    const int n = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+Tiles tiles_of(const usl_ctx* c, int w, int rows, int k_steps, bool direct) {
+    const int by_64 = (rows + 63) / 64, by_128 = (rows + 127) / 128;
+    const int n = rows <= 32 ? 32 : rows <= 64 || (direct && by_64 * 8 <= by_128 * 14) ? 64 : 128;
     const bool wide = w > 128 && (int64_t)((w + 255) / 256) * ((rows + n - 1) / n) * (k_steps / 16) >= c->num_cu;
     return wide ? Tiles{256, n} : Tiles{128, 128};
 }
@@ -384,8 +387,9 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
     if (most > padded((size_t)c->max_b)) most = padded((size_t)c->max_b);
     if (most > 32768) most = 32768;   // a row is a grid dimension
     const int k_steps = 2 * a.dp / DEPTH;
+    const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
     auto cut = [&](Grad& g, int rows) {   // a workgroup to a compute unit; at least four steps each
-        const Tiles t = tiles_of(c, g.w, rows, k_steps);
+        const Tiles t = tiles_of(c, g.w, rows, k_steps, direct);
         g.tiles_m = (g.w + t.m - 1) / t.m;
         g.tiles_n = (rows + t.n - 1) / t.n;
         const int tiles = g.tiles_m * g.tiles_n, want = c->num_cu / tiles, room = (k_steps + 3) / 4;   // (one more than there is room for takes another round)
@@ -420,7 +424,6 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         }
         if (!a.grad_e) continue;
         const Tiles t = cut(a, a.rows);
-        const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
         if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, 4, true>(c, a) : grad_e<T, 128, 128, 4, 3, false>(c, a)));
         else if (t.n == 32) USL_TRY((direct ? grad_e<T, 256, 32, 2, 4, true>(c, a) : grad_e<T, 256, 32, 2, 3, false>(c, a)));
         else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, 4, true>(c, a) : grad_e<T, 256, 64, 4, 3, false>(c, a)));
