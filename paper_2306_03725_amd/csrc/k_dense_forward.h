@@ -300,8 +300,9 @@ usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
 //   float32: 169 x 256 -> 16512  64 x 64 40, 128 x 128 72;  1000 x 500 -> 20000  348 and 406;  512 x 768 -> 32768  128 x 256 398, 64 x 64 406
 // At most 16 instances: tiles of 64 x 16 where there is one for every compute unit: 1 x -> 32768 19.2, rows straight into fragments 21.6; 8 x -> 16384 9.8 and 11.6; 8 x -> 8192
 // 7.2 and 7.1; 8 x -> 32768 float32 42.5 and 51.4; 1 x 512 -> 65536 from 8 bits 10.0 and 10.5.
-// Rows straight into fragments otherwise, and for up to two fragments to a compute unit, whose wavefronts then share K: 48 x 1792 -> 64 6.9, 32 x 64 14.1; 58 x 1083 -> 1675
-// float32 17 and 39; 100 x 1000 -> 1000 8.9 and 9.7; not 200 x 512 -> 1024 (832 fragments) 7.6 and 6.3.
+// Rows straight into fragments otherwise, and for up to two fragments to a compute unit (four in float32), whose wavefronts then share K: 48 x 1792 -> 64 6.9, 32 x 64 14.1;
+// 100 x 1000 -> 1000 8.9 and 9.7; not 200 x 512 -> 1024 (832 fragments) 7.6 and 6.3.  float32: 64 x 880 -> 2471 15.4 and 24.5, 200 x 512 -> 1024 12.9 and 15.2; not
+// 333 x 512 -> 1024 (1344) 18.6 and 15.4.
 template <typename T, typename TO, int MATS, int ACT>
 usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
     constexpr int FEW = MATS == 1 ? 128 : 64, MANY = MATS == 1 ? 256 : 128;
@@ -309,7 +310,7 @@ usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
     const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
     auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
     if (direct && a.b <= 16 && tiles(FEW, 16) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
-    if (a.b <= 16 || tiles(16, 16) <= 2 * c->num_cu) {
+    if (a.b <= 16 || tiles(16, 16) <= (SLOW ? 4 : 2) * c->num_cu) {
         hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16), (unsigned)((a.b + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
