@@ -14,6 +14,7 @@ struct Forward {
     void *x, *gate, *up;       // [b][d]; gate, up may be null
     int d, b, row_bytes;       // of a row of V and e
     int tiles_d, tiles_b;
+    int whole;                 // results' rows consist of whole 64-byte pieces of memory
 };
 
 // What 8-bit integers' sums are multiplied by: a lane's N neighbours of each matrix
@@ -29,12 +30,14 @@ struct Scales {
     }
 };
 // gate and up go past the caches, which have V and e to keep: 512 x 768 -> 32768 bfloat16 74 us, so 67 (x too: 68); the results from 8-bit integers too: 1024 x 512 ->
-// 65536 67 and 59, 500 x 750 -> 32768 gated 60 and 58.
+// 65536 67 and 59, 500 x 750 -> 32768 gated 60 and 58.  Where rows of the results end inside 64 bytes of memory, two tiles write them, and past the caches that is two
+// writes of a part; through the caches, with the two tiles on one chiplet, it is one: 942 x 128 -> 65033 bfloat16 250 us, on one chiplet 218, and through the caches 156;
+// 512 x 768 -> 32760 96, 83, 76.  From 8 bits past them all the same: 942 x 512 -> 65033 gated 125, through them 148 (on two chiplets 142 and 149).
 // 16 instances' values of WD neighbouring activations, a lane N of one instance's, to rows of memory: through LDS, so that a store takes whole lines of it.
 // (16 rows of 64 bytes to a store, the other half of every line by the next one: 512 x 768 -> 32768 bfloat16, three outputs, 85 us, and with more between the
 // two 98; in whole lines 73.)  `mine`: the wavefront's own LDS.
 template <typename TO, int WD, bool PAST_CACHES, int N>
-__device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N], int i0, int b, int d0, int d) {
+__device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N], int i0, int b, int d0, int d, bool past) {
     constexpr int ROW = WD * (int)sizeof(TO), PITCH = ROW + 16, EACH = 16 / (int)sizeof(TO), GROUPS = ROW / 16;
     static_assert(N * 4 == WD, "four lanes share a row");
     const int l = (int)threadIdx.x & 63;
@@ -57,8 +60,11 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
             TO* p = to + (size_t)i * d + c;
             if (d - c >= EACH) {
                 typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
-                if (PAST_CACHES) __builtin_nontemporal_store(__builtin_bit_cast(Words, w), reinterpret_cast<Words*>(p));
-                else *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
+                if (PAST_CACHES && past) {   // (the two lines around it keep the compiler from making one store of the two)
+                    asm volatile("; past the caches" ::: "memory");
+                    __builtin_nontemporal_store(__builtin_bit_cast(Words, w), reinterpret_cast<Words*>(p));
+                    asm volatile("; past the caches" ::: "memory");
+                } else *reinterpret_cast<Words*>(p) = __builtin_bit_cast(Words, w);
             } else {
                 TO one[EACH];
                 __builtin_memcpy(one, &w, 16);
@@ -85,9 +91,11 @@ k_dense_forward(Forward a) {
     using SE = StageKC<BB, KB, 1, WAVES>;
     constexpr int STEP = SV::BYTES + SE::BYTES, LOADS = (TOGETHER ? 1 : MATS) * SQ::LOADS + SE::LOADS;
     extern __shared__ __align__(1024) char lds[];
-    // Workgroups go to the chiplets in turn: the tiles of one piece of V, which share its rows, go to one of them, one after the other.
-    const int turn = (int)blockIdx.x >> 3, td = turn / a.tiles_b * 8 + ((int)blockIdx.x & 7), tb = turn % a.tiles_b;
-    if (td >= a.tiles_d) return;
+    // Workgroups go to the chiplets in turn: the tiles of one piece of V, which share its rows, go to one of them, one after the other; so do those of its neighbours where
+    // a piece of memory holds results of two tiles, to be one write of the chiplet's cache.
+    const int turn = (int)blockIdx.x >> 3, xcd = (int)blockIdx.x & 7, tb = turn % a.tiles_b, nth = turn / a.tiles_b;
+    const int td = a.whole ? nth * 8 + xcd : (int)((int64_t)xcd * a.tiles_d >> 3) + nth;
+    if (td >= (a.whole ? a.tiles_d : (int)((int64_t)(xcd + 1) * a.tiles_d >> 3))) return;
     const int d0 = td * BD, b0 = tb * BB, wave = (int)threadIdx.x >> 6, wd = wave % WAVES_D * (BD / WAVES_D), wb = wave / WAVES_D * (BB / WAVES_B);
     const int rows_d = min(a.d - d0, BD), rows_b = min(a.b - b0, BB);
     const uint32_t pitch = (uint32_t)a.row_bytes;
@@ -190,6 +198,7 @@ k_dense_forward(Forward a) {
     char* mine = lds + wave * 16 * (WD * (int)sizeof(TO) + 16);
     Scales<T, MATS, N> scales;
     scales.load(a, c0 + (l >> 4) * N);
+    const bool past = sizeof(T) == 1 || a.whole;
     __syncthreads();   // the last step has been read
 #pragma unroll
     for (int g = 0; g < FB; ++g) {
@@ -203,15 +212,15 @@ k_dense_forward(Forward a) {
                 if (sizeof(T) == 1) v[q][j] *= e_scale * scales.v[q][j];
             }
         if (MATS == 1) {
-            put_tile<TO, WD, true>(mine, (TO*)a.x, v[0], i0 + g * 16, a.b, c0, a.d);
+            put_tile<TO, WD, true>(mine, (TO*)a.x, v[0], i0 + g * 16, a.b, c0, a.d, past);
             continue;
         }
         float x[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
-        put_tile<TO, WD, sizeof(T) == 1>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d);
-        if (a.gate) put_tile<TO, WD, true>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d);
-        if (a.up) put_tile<TO, WD, true>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d);
+        put_tile<TO, WD, sizeof(T) == 1>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d, past);
+        if (a.gate) put_tile<TO, WD, true>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d, past);
+        if (a.up) put_tile<TO, WD, true>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d, past);
     }
 }
 
@@ -298,24 +307,27 @@ usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
 //   128 x -> 32768  128 x 128 29.5, 64 x 64 37        64 x -> 32768   64 x 64 25, 128 x 128 27
 //   512 x -> 4096   64 x 64 14, 128 x 128 18          100 x 1000 -> 3000  32 x 64 9.8, 64 x 64 12.1
 //   float32: 169 x 256 -> 16512  64 x 64 40, 128 x 128 72;  1000 x 500 -> 20000  348 and 406;  512 x 768 -> 32768  128 x 256 398, 64 x 64 406
+//   from 8 bits, rows of at most 768: 942 x 128 -> 65536  128 x 128 74, 128 x 256 87;  942 x 512 -> 65536  117 and 125;  942 x 768 -> 65536  161 and 164;  942 x 2048 -> 65536  322 and 308
 // At most 16 instances: tiles of 64 x 16 where there is one for every compute unit: 1 x -> 32768 19.2, rows straight into fragments 21.6; 8 x -> 16384 9.8 and 11.6; 8 x -> 8192
 // 7.2 and 7.1; 8 x -> 32768 float32 42.5 and 51.4; 1 x 512 -> 65536 from 8 bits 10.0 and 10.5.
 // Rows straight into fragments otherwise, and for up to two fragments to a compute unit (four in float32), whose wavefronts then share K: 48 x 1792 -> 64 6.9, 32 x 64 14.1;
 // 100 x 1000 -> 1000 8.9 and 9.7; not 200 x 512 -> 1024 (832 fragments) 7.6 and 6.3.  float32: 64 x 880 -> 2471 15.4 and 24.5, 200 x 512 -> 1024 12.9 and 15.2; not
 // 333 x 512 -> 1024 (1344) 18.6 and 15.4.
 template <typename T, typename TO, int MATS, int ACT>
-usl_status launch_forward(usl_ctx* c, const Forward& a, const char* what) {
+usl_status launch_forward(usl_ctx* c, Forward a, const char* what) {
     constexpr int FEW = MATS == 1 ? 128 : 64, MANY = MATS == 1 ? 256 : 128;
     constexpr bool SLOW = sizeof(T) == 4;
     const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
+    a.whole = ((size_t)a.d * sizeof(TO) | (uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.up) % 64 == 0;
     auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
     if (direct && a.b <= 16 && tiles(FEW, 16) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
     if (a.b <= 16 || tiles(16, 16) <= (SLOW ? 4 : 2) * c->num_cu) {
         hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16), (unsigned)((a.b + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
+    const bool short_ones = sizeof(T) == 1 && MATS == 2 && a.row_bytes <= 768;
     auto cost = [&](int d, int b, double rate) { return (double)((tiles(d, b) + c->num_cu - 1) / c->num_cu) * d * b / rate; };
-    const double by_many = direct ? cost(MANY, 256, 1.0) : INFINITY, by_128 = cost(128, 128, SLOW ? 1.0 : 0.8), by_64 = cost(64, 64, SLOW ? 0.97 : 0.59),
+    const double by_many = direct ? cost(MANY, 256, 1.0) : INFINITY, by_128 = cost(128, 128, SLOW ? 1.0 : short_ones ? 1.05 : 0.8), by_64 = cost(64, 64, SLOW ? 0.97 : 0.59),
                  by_32 = MATS == 2 ? cost(32, 64, SLOW ? 0.9 : 0.42) : INFINITY;
     if (by_many <= by_128 && by_many <= by_64 && by_many <= by_32) return launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, true>(c, a, what);
     if (by_128 <= by_64 && by_128 <= by_32)
