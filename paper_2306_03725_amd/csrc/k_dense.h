@@ -188,11 +188,15 @@ struct StageKO {
             to_lds(lds + (uint32_t)((t * WAVES + (int)(threadIdx.x >> 6)) * 1024), buffer, k < depth && g < width ? (uint32_t)k * (uint32_t)pitch + (uint32_t)g : NOWHERE);
         }
     }
-    // (before: bytes of a row before the first column)
+    // The same through registers.  Columns behind a row's end come out as the next row's numbers, as long as there is a next row, and as zeros in the matrix's last step
+    // (a column has its own results; cut off in every step: 20 x 2014 -> 36853 backward, float32, 654 us, so 376).  before: bytes of a row before the first column
     static __device__ __forceinline__ void fetch(i32x4 (&held)[LOADS], const char* from, int depth, size_t pitch, int width, int before) {
-        if (depth >= DEPTH && width >= ROW) {
+        if (depth > DEPTH && pitch >= 16) {
 #pragma unroll
-            for (int t = 0; t < LOADS; ++t) held[t] = *reinterpret_cast<const i32x4_any*>(from + (size_t)row_of(t) * pitch + group_of(t) * 16);
+            for (int t = 0; t < LOADS; ++t) {
+                const int g = group_of(t) * 16;
+                held[t] = *reinterpret_cast<const i32x4_any*>(from + (size_t)row_of(t) * pitch + (g < width ? g : 0));
+            }
         } else {
 #pragma unroll
             for (int t = 0; t < LOADS; ++t) {
