@@ -106,7 +106,7 @@ struct StageKC {
     static __device__ __forceinline__ int first_of(int t) { return (t * WAVES + (int)(threadIdx.x >> 6)) * AT_ONCE % ROWS; }
     static __device__ __forceinline__ int row_of(int t) { return first_of(t) + (int)(threadIdx.x & 63) / (KB / 16); }
     static __device__ __forceinline__ int group_of(int t) { return place_of<KB, SPREAD>(row_of(t), (int)(threadIdx.x & 63) % (KB / 16)); }
-    // from: row 0 of the tile at this step's first byte; rows: how many there are; left: bytes of K from here to the end (multiples of 16, as from's address)
+    // from: row 0 of the tile at this step's first byte; rows: how many there are; left: bytes of K from here to the end, a multiple of 16 or KB and more; from's address a multiple of 4
     static __device__ __forceinline__ void direct(uint32_t lds, const char* from, int rows, uint32_t pitch, int left) {
         const i32x4 buffer = buffer_at(from);
 #pragma unroll

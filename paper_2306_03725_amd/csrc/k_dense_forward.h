@@ -76,13 +76,18 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
     }
 }
 
-// A tile of BD activations of BB instances.  DIRECT: rows and bases are multiples of 16 bytes; STAGES steps of K then have room in LDS, one being
-// multiplied and the others on their way.  Else the tiles come through registers, asked for two steps ahead.
-template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
+// How rows come into LDS.  DIRECT: they and their bases are multiples of 16 bytes; STAGES steps of K then have room in LDS, one being multiplied and the others on their
+// way.  WORDS: of 4; the same for whole steps, and what is left of a row through registers behind them.  Else everything through registers, asked for two steps ahead.
+// us, in words and through registers, and with a row of a few numbers more, directly: 60 x 1830 -> 7059 bfloat16 17.1, 34.2, 16.2; 47 x 1990 -> 11048 float32 79, 111, 78;
+// 910 x 940 -> 1147 from 8 bits 12.8, 16.0, 12.1; 773 x 542 -> 4324 bfloat16 32.2, 33.5, 25.0.
+enum { REGISTERS, DIRECT, WORDS };
+
+// A tile of BD activations of BB instances.
+template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, int HOW>
 __global__ void __launch_bounds__(64 * WAVES_D * WAVES_B, 2)   // (two wavefronts to a SIMD: sums and fragments in 256 registers)
 k_dense_forward(Forward a) {
     constexpr int WAVES = WAVES_D * WAVES_B, KB = 64, FD = BD / WAVES_D / 16, FB = BB / WAVES_B / 16;
-    static_assert(DIRECT || STAGES == 2, "two sets of registers");
+    static_assert(HOW != REGISTERS || STAGES == 2, "two sets of registers");
     using Acc = typename Core<T>::Acc;
     // V's rows, gate's before up's; a lane's neighbours of all fragments are neighbours.  TOGETHER: the rows of one matrix are too few for all wavefronts.
     constexpr bool TOGETHER = BD < 16 * WAVES;
@@ -109,9 +114,38 @@ k_dense_forward(Forward a) {
         for (int f = 0; f < FD; ++f)
 #pragma unroll
             for (int h = 0; h < FB; ++h) acc[q][f][h] = Acc{0, 0, 0, 0};
-    const int steps = (a.row_bytes + KB - 1) / KB;
+    const int steps = HOW == WORDS ? a.row_bytes / KB : (a.row_bytes + KB - 1) / KB;
     const int lane_v = SV::lane(wd), lane_e = SE::lane(wb);
-    if constexpr (DIRECT) {
+    struct Held { i32x4 v[TOGETHER ? 1 : MATS][SQ::LOADS], e[SE::LOADS]; };
+    auto ask = [&](Held& h, int s) {
+        const int at = s * KB, left = a.row_bytes - at;
+        if (left <= 0) return;
+        const char* const from[2] = {V[0] + at, V[1] + at};
+        if constexpr (TOGETHER) SQ::fetch_two(h.v[0], from, BD, rows_d, pitch, left, at);
+        else
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) SQ::fetch(h.v[q], from[q], rows_d, pitch, left, at);
+        SE::fetch(h.e, e + at, rows_b, pitch, left, at);
+    };
+    auto put = [&](const Held& h, char* to) {
+#pragma unroll
+        for (int q = 0; q < (TOGETHER ? 1 : MATS); ++q) SQ::put(to + q * SQ::BYTES, h.v[q]);
+        SE::put(to + SV::BYTES, h.e);
+    };
+    auto multiply = [&](const char* from) {
+        i32x4 eb[FB];
+#pragma unroll
+        for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + SV::BYTES, lane_e, f);
+#pragma unroll
+        for (int q = 0; q < MATS; ++q)
+#pragma unroll
+            for (int f = 0; f < FD; ++f) {
+                const i32x4 v = SV::frag(from + q * (BD * KB), lane_v, f);
+#pragma unroll
+                for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
+            }
+    };
+    if constexpr (HOW != REGISTERS) {
         constexpr int GROUPS = 2, Y = MATS * FD / GROUPS;   // a matrix, or half of one's fragments
         auto place = [&](int s) { return lds + s % STAGES * STEP; };
         walk<FB, GROUPS, Y, STAGES>(
@@ -144,38 +178,18 @@ k_dense_forward(Forward a) {
                         to = Core<T>::mul(y[f], x[h], to);
                     }
             });
+        if (HOW == WORDS && steps * KB < a.row_bytes) {
+            Held rest;
+            ask(rest, steps);
+            __syncthreads();   // the last whole step has been read
+            put(rest, lds);
+            __syncthreads();
+            multiply(lds);
+        }
     } else {
-        struct Held { i32x4 v[TOGETHER ? 1 : MATS][SQ::LOADS], e[SE::LOADS]; };
         Held one, two;   // steps s + 1 and s + 2
-        auto multiply = [&](const char* from) {
-            i32x4 eb[FB];
-#pragma unroll
-            for (int f = 0; f < FB; ++f) eb[f] = SE::frag(from + SV::BYTES, lane_e, f);
-#pragma unroll
-            for (int q = 0; q < MATS; ++q)
-#pragma unroll
-                for (int f = 0; f < FD; ++f) {
-                    const i32x4 v = SV::frag(from + q * (BD * KB), lane_v, f);
-#pragma unroll
-                    for (int g = 0; g < FB; ++g) acc[q][f][g] = Core<T>::mul(v, eb[g], acc[q][f][g]);
-                }
-        };
-        auto ask = [&](Held& h, int s) {
-            if (s >= steps) return;
-            const int at = s * KB, left = a.row_bytes - at;
-            const char* const from[2] = {V[0] + at, V[1] + at};
-            if constexpr (TOGETHER) SQ::fetch_two(h.v[0], from, BD, rows_d, pitch, left, at);
-            else
-#pragma unroll
-                for (int q = 0; q < MATS; ++q) SQ::fetch(h.v[q], from[q], rows_d, pitch, left, at);
-            SE::fetch(h.e, e + at, rows_b, pitch, left, at);
-        };
         auto place = [&](const Held& h, int s) {
-            if (s >= steps) return;
-            char* to = lds + (s & 1) * STEP;
-#pragma unroll
-            for (int q = 0; q < (TOGETHER ? 1 : MATS); ++q) SQ::put(to + q * SQ::BYTES, h.v[q]);
-            SE::put(to + SV::BYTES, h.e);
+            if (s < steps) put(h, lds + (s & 1) * STEP);
         };
         ask(two, 0);
         ask(one, 1);
@@ -288,10 +302,10 @@ k_dense_few(Forward a) {
     }
 }
 
-template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, bool DIRECT>
+template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, int HOW>
 usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
     constexpr int BYTES = STAGES * (MATS * BD + BB) * 64;
-    const auto kernel = k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, STAGES, DIRECT>;
+    const auto kernel = k_dense_forward<T, TO, MATS, ACT, BD, BB, WAVES_D, WAVES_B, STAGES, HOW>;
     a.tiles_d = (a.d + BD - 1) / BD;
     a.tiles_b = (a.b + BB - 1) / BB;
     const dim3 grid((unsigned)((a.tiles_d + 7) / 8 * 8 * a.tiles_b)), block(64 * WAVES_D * WAVES_B);
@@ -317,25 +331,33 @@ template <typename T, typename TO, int MATS, int ACT>
 usl_status launch_forward(usl_ctx* c, Forward a, const char* what) {
     constexpr int FEW = MATS == 1 ? 128 : 64, MANY = MATS == 1 ? 256 : 128;
     constexpr bool SLOW = sizeof(T) == 4;
-    const bool direct = (a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e) % 16 == 0;
+    const uintptr_t rows = a.row_bytes | (uintptr_t)a.V[0] | (uintptr_t)a.V[MATS - 1] | (uintptr_t)a.e;
+    const int how = rows % 16 == 0 ? DIRECT : rows % 4 == 0 ? WORDS : REGISTERS;
     a.whole = ((size_t)a.d * sizeof(TO) | (uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.up) % 64 == 0;
     auto tiles = [&](int d, int b) { return (int64_t)((a.d + d - 1) / d) * ((a.b + b - 1) / b); };
-    if (direct && a.b <= 16 && tiles(FEW, 16) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, true>(c, a, what);
+    if (how == DIRECT && a.b <= 16 && tiles(FEW, 16) >= c->num_cu) return launch_tiles<T, TO, MATS, ACT, FEW, 16, 4, 1, 5, DIRECT>(c, a, what);
     if (a.b <= 16 || tiles(16, 16) <= (SLOW ? 4 : 2) * c->num_cu) {
         hipLaunchKernelGGL((k_dense_few<T, TO, MATS, ACT, 4>), dim3((unsigned)((a.d + 15) / 16), (unsigned)((a.b + 15) / 16)), dim3(256), 0, c->stream, a);
         return usl_check_launch(c, what);
     }
     const bool short_ones = sizeof(T) == 1 && MATS == 2 && a.row_bytes <= 768;
     auto cost = [&](int d, int b, double rate) { return (double)((tiles(d, b) + c->num_cu - 1) / c->num_cu) * d * b / rate; };
-    const double by_many = direct ? cost(MANY, 256, 1.0) : INFINITY, by_128 = cost(128, 128, SLOW ? 1.0 : short_ones ? 1.05 : 0.8), by_64 = cost(64, 64, SLOW ? 0.97 : 0.59),
+    const double by_many = how != REGISTERS ? cost(MANY, 256, 1.0) : INFINITY, by_128 = cost(128, 128, SLOW ? 1.0 : short_ones ? 1.05 : 0.8), by_64 = cost(64, 64, SLOW ? 0.97 : 0.59),
                  by_32 = MATS == 2 ? cost(32, 64, SLOW ? 0.9 : 0.42) : INFINITY;
-    if (by_many <= by_128 && by_many <= by_64 && by_many <= by_32) return launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, true>(c, a, what);
+    if (by_many <= by_128 && by_many <= by_64 && by_many <= by_32)
+        return how == DIRECT ? launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, DIRECT>(c, a, what) : launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, WORDS>(c, a, what);
     if (by_128 <= by_64 && by_128 <= by_32)
-        return direct ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, false>(c, a, what);
+        return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, DIRECT>(c, a, what)
+               : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, WORDS>(c, a, what)
+                              : launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, REGISTERS>(c, a, what);
     if constexpr (MATS == 2)
         if (by_32 < by_64)
-            return direct ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, false>(c, a, what);
-    return direct ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, true>(c, a, what) : launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, false>(c, a, what);
+            return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, DIRECT>(c, a, what)
+                   : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, WORDS>(c, a, what)
+                                  : launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, REGISTERS>(c, a, what);
+    return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, DIRECT>(c, a, what)
+           : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, WORDS>(c, a, what)
+                          : launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, REGISTERS>(c, a, what);
 }
 
 }  // namespace dense

@@ -90,6 +90,13 @@ def test_forward_of_large_tiles(b, w, d, storage):
     forward_case(b, w, d, storage, 0)
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("b,w,d,shift", [(300, 70, 32770, 0), (300, 30, 32768, 0), (300, 64, 32768, 2), (130, 70, 16400, 0), (257, 201, 20001, 0), (200, 70, 9000, 2), (70, 70, 3001, 0),
+                                         (70, 2, 3001, 0), (70, 64, 3001, 2), (100, 130, 1500, 0)])
+def test_forward_of_rows_of_words(b, w, d, shift, storage):
+    forward_case(b, w, d, storage, b % 2, shift=shift)
+
+
 @pytest.mark.parametrize("b", [4, 40])
 def test_forward_keeps_nothing_if_not_asked(b):
     forward_case(b, 50, 60, "bf16", 1, keep=False)

@@ -75,7 +75,8 @@ def numbers(rows, w, seed, shift=0):
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("b,w,d,shift", [(1, 1, 1, 0), (1, 64, 16, 0), (2, 63, 17, 0), (16, 65, 15, 1), (16, 1024, 100, 0), (17, 128, 64, 0), (33, 127, 65, 3), (70, 129, 200, 0),
-                                         (130, 48, 300, 16), (5, 750, 70, 0), (64, 750, 64, 2), (1, 65536, 5, 0), (20, 65536, 20, 0), (140, 96, 16500, 0), (9, 80, 33000, 0), (16, 256, 16400, 0), (130, 64, 65600, 0)])
+                                         (130, 48, 300, 16), (5, 750, 70, 0), (64, 750, 64, 2), (1, 65536, 5, 0), (20, 65536, 20, 0), (140, 96, 16500, 0), (9, 80, 33000, 0), (16, 256, 16400, 0), (130, 64, 65600, 0), (300, 100, 65601, 0),
+                                         (300, 36, 33000, 4), (70, 100, 3001, 0), (70, 1004, 500, 8), (200, 68, 9000, 0)])
 def test_products(b, w, d, shift, storage):
     dtype = TYPES[storage]
     q, s = numbers(b, w, 1, shift)
