@@ -83,6 +83,9 @@ __device__ __forceinline__ i32x4 sixteen(const char* p, int bytes, int before) {
     return __builtin_bit_cast(i32x4, r);
 }
 
+// How rows come into LDS: through registers, from any address; or straight, from multiples of 16 bytes, or of 4 but for what ends inside 16
+enum { REGISTERS, DIRECT, WORDS };
+
 // ---- KC: ROWS rows of KB (128 or 64) bytes of K
 // The row of a tile that fragment f's row i is.  SPREAD fragments side by side: a lane's four neighbours of each of them are 4 * SPREAD neighbours.
 template <int SPREAD>

@@ -80,8 +80,6 @@ __device__ __forceinline__ void put_tile(char* mine, TO* to, const float (&v)[N]
 // way.  WORDS: of 4; the same for whole steps, and what is left of a row through registers behind them.  Else everything through registers, asked for two steps ahead.
 // us, in words and through registers, and with a row of a few numbers more, directly: 60 x 1830 -> 7059 bfloat16 17.1, 34.2, 16.2; 47 x 1990 -> 11048 float32 79, 111, 78;
 // 910 x 940 -> 1147 from 8 bits 12.8, 16.0, 12.1; 773 x 542 -> 4324 bfloat16 32.2, 33.5, 25.0.
-enum { REGISTERS, DIRECT, WORDS };
-
 // A tile of BD activations of BB instances.
 template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int WAVES_D, int WAVES_B, int STAGES, int HOW>
 __global__ void __launch_bounds__(64 * WAVES_D * WAVES_B, 2)   // (two wavefronts to a SIMD: sums and fragments in 256 registers)

@@ -201,16 +201,16 @@ k_gated_grad_v(Grad a) {
     }
 }
 
-// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  Tiles of MT x NT, a wavefront 64 x 16 * FN of it.  DIRECT: V's rows and bases are
-// multiples of 16 bytes; else V comes through registers, asked for two steps ahead and put into LDS one step ahead.
-template <typename T, int MT, int NT, int FN, int STAGES, bool DIRECT>
+// Sums of grad_e over a piece of [2][d]: [w] along m, the instances along n.  Tiles of MT x NT, a wavefront 64 x 16 * FN of it.  V comes straight into
+// LDS, with rows and bases that are multiples of 4 bytes all but the steps at its end (20 x 2014 -> 36853 float32 376 us, so 344); else through registers, asked for two steps ahead and put into LDS one step ahead.
+template <typename T, int MT, int NT, int FN, int STAGES, int HOW>
 __global__ void __launch_bounds__(MT * NT / (16 * FN), 2)
 k_gated_grad_e(Grad a) {
     constexpr int P = PARTS<T>, F = 4, WAVES = MT / 64 * (NT / (FN * 16));
     using SV = StageKO<T, MT, WAVES>;
     using SG = StageKC<NT, 64, 1, WAVES>;
-    constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (DIRECT ? SV::LOADS : 0) + P * SG::LOADS;
-    static_assert(DIRECT || STAGES == 3, "two steps ahead");
+    constexpr int STEP = SV::BYTES + P * SG::BYTES, LOADS = (HOW != REGISTERS ? SV::LOADS : 0) + P * SG::LOADS;
+    static_assert(HOW != REGISTERS || STAGES == 3, "two steps ahead");
     extern __shared__ __align__(1024) char lds[];
     int tile, piece;
     if (!tile_of(a.tiles_m * a.tiles_n, a.splits, tile, piece)) return;
@@ -241,7 +241,12 @@ k_gated_grad_e(Grad a) {
         if (s >= steps) return;
         const int k = (first + s) * SV::DEPTH, which = k >= a.dp, row = k - which * a.dp;   // rows behind V's end meet zeros of G, and are not read
         const char* V = (const char*)a.V[which] + (size_t)min(row, a.d - 1) * pitch_v + (size_t)m0 * sizeof(T);
-        if constexpr (DIRECT) SV::direct(lds_at(place(s)), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
+        if (HOW == WORDS && a.d - row <= SV::DEPTH) {
+            Held last;
+            landed<0>();   // (arrived() counts on as many loads of every step behind its own: here they are fewer, and what lies before is there)
+            SV::fetch(last.v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
+            SV::put(place(s), last.v);
+        } else if (HOW != REGISTERS) SV::direct(lds_at(place(s)), V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T));
         else SV::fetch(h->v, V, a.d - row, pitch_v, (a.w - m0) * (int)sizeof(T), m0 * (int)sizeof(T));
     };
     constexpr int GROUPS = P > 1 ? P : 2, Y = P * FN / GROUPS;
@@ -259,7 +264,7 @@ k_gated_grad_e(Grad a) {
 #pragma unroll
             for (int f = 0; f < F; ++f) acc[f][(g * Y + h) % FN] = Core<T>::mul(x[f], y[h], acc[f][(g * Y + h) % FN]);
     };
-    if constexpr (DIRECT) {
+    if constexpr (HOW != REGISTERS) {
         walk<F, GROUPS, Y, STAGES>(
             steps, [&](int s) { arrived<STAGES, LOADS>(s, steps); },
             [&](int s) {
@@ -341,19 +346,25 @@ usl_status grad_v(usl_ctx* c, Grad a) {
     return usl_check_launch(c, "gated_block_backward");
 }
 
-template <typename T, int MT, int NT, int FN, int STAGES, bool DIRECT>
-usl_status grad_e(usl_ctx* c, Grad a) {
+template <typename T, int MT, int NT, int FN, int STAGES, int HOW>
+usl_status grad_e_tiles(usl_ctx* c, const Grad& a) {
     constexpr int BYTES = STAGES * (MT + PARTS<T> * NT) * 64;
-    USL_TRY(lds_for(c, k_gated_grad_e<T, MT, NT, FN, STAGES, DIRECT>, BYTES));
-    hipLaunchKernelGGL((k_gated_grad_e<T, MT, NT, FN, STAGES, DIRECT>), dim3(tiles_grid(a.tiles_m * a.tiles_n, a.splits)), dim3(MT * NT / (16 * FN)), BYTES, c->stream, a);
+    USL_TRY(lds_for(c, k_gated_grad_e<T, MT, NT, FN, STAGES, HOW>, BYTES));
+    hipLaunchKernelGGL((k_gated_grad_e<T, MT, NT, FN, STAGES, HOW>), dim3(tiles_grid(a.tiles_m * a.tiles_n, a.splits)), dim3(MT * NT / (16 * FN)), BYTES, c->stream, a);
     return usl_check_launch(c, "gated_block_backward");
+}
+
+template <typename T, int MT, int NT, int FN>
+usl_status grad_e(usl_ctx* c, const Grad& a, int how) {
+    if (how == DIRECT) return grad_e_tiles<T, MT, NT, FN, 4, DIRECT>(c, a);
+    return how == WORDS ? grad_e_tiles<T, MT, NT, FN, 4, WORDS>(c, a) : grad_e_tiles<T, MT, NT, FN, 3, REGISTERS>(c, a);
 }
 
 // Tiles of grad_e.  Instances 32 or 64 at a time where there are no more, and 64 where V comes straight into LDS and they leave out an eighth of what 128 at a time
 // would multiply; 256 columns of w where every compute unit then has at least 16 steps to go, else 128, which share the work among twice the workgroups and leave
 // half the sums.  (Backward of 300 x 200 -> 1000 float32, 25 us, 7 more with 256 columns; of 1 x 130 -> 45688 float32 with 32 instances at a time 117 us, with 64 at a time 127;
 // with 64 and 128 at a time: 155 x 256 -> 55424 float32 221 and 244, bfloat16 140 and 145, 300 x 384 -> 16384 float32 193 and 204, 512 x 768 -> 16384 482 and 457,
-// 200 x 301 -> 30001, V through registers, 458 and 288.)
+// 150 x 301 -> 30001 bfloat16, V through registers, 171 and 129.)
 struct Tiles { int m, n; };
 Tiles tiles_of(const usl_ctx* c, int w, int rows, int k_steps, bool direct) {
     const int by_64 = (rows + 63) / 64, by_128 = (rows + 127) / 128;
@@ -387,9 +398,10 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
     if (most > padded((size_t)c->max_b)) most = padded((size_t)c->max_b);
     if (most > 32768) most = 32768;   // a row is a grid dimension
     const int k_steps = 2 * a.dp / DEPTH;
-    const bool direct = (a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1]) % 16 == 0;
+    const uintptr_t rows_at = a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1];
+    const int how = rows_at % 16 == 0 ? DIRECT : rows_at % 4 == 0 && a.w * ES >= 16 ? WORDS : REGISTERS;   // (16 bytes from a row on end in the next one at the latest)
     auto cut = [&](Grad& g, int rows) {   // a workgroup to a compute unit; at least four steps each
-        const Tiles t = tiles_of(c, g.w, rows, k_steps, direct);
+        const Tiles t = tiles_of(c, g.w, rows, k_steps, how != REGISTERS);
         g.tiles_m = (g.w + t.m - 1) / t.m;
         g.tiles_n = (rows + t.n - 1) / t.n;
         const int tiles = g.tiles_m * g.tiles_n, want = c->num_cu / tiles, room = (k_steps + 3) / 4;   // (one more than there is room for takes another round)
@@ -424,10 +436,10 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         }
         if (!a.grad_e) continue;
         const Tiles t = cut(a, a.rows);
-        if (t.m == 128) USL_TRY((direct ? grad_e<T, 128, 128, 4, 4, true>(c, a) : grad_e<T, 128, 128, 4, 3, false>(c, a)));
-        else if (t.n == 32) USL_TRY((direct ? grad_e<T, 256, 32, 2, 4, true>(c, a) : grad_e<T, 256, 32, 2, 3, false>(c, a)));
-        else if (t.n == 64) USL_TRY((direct ? grad_e<T, 256, 64, 4, 4, true>(c, a) : grad_e<T, 256, 64, 4, 3, false>(c, a)));
-        else USL_TRY((direct ? grad_e<T, 256, 128, 4, 4, true>(c, a) : grad_e<T, 256, 128, 4, 3, false>(c, a)));
+        if (t.m == 128) USL_TRY((grad_e<T, 128, 128, 4>(c, a, how)));
+        else if (t.n == 32) USL_TRY((grad_e<T, 256, 32, 2>(c, a, how)));
+        else if (t.n == 64) USL_TRY((grad_e<T, 256, 64, 4>(c, a, how)));
+        else USL_TRY((grad_e<T, 256, 128, 4>(c, a, how)));
         const size_t n = (size_t)a.b * a.w;
         hipLaunchKernelGGL(k_gated_join, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, c->stream, a.sums, a.grad_e + (size_t)i0 * a.w, n, a.splits);
         USL_TRY(usl_check_launch(c, what));

@@ -168,7 +168,8 @@ def test_backward(b, w, d, storage):
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("b,w,d", [(5, 264, 33000), (32, 301, 33000), (33, 264, 33000), (64, 299, 33001), (150, 500, 8100), (130, 384, 16400), (17, 513, 8192),
-                                   (161, 264, 33000), (300, 520, 8200), (40, 71, 9001), (20, 334, 9001), (140, 3, 9001)])
+                                   (161, 264, 33000), (300, 520, 8200), (40, 71, 9001), (20, 334, 9001), (140, 3, 9001), (140, 4, 9001),
+                                   (40, 270, 33023), (161, 278, 33100), (9, 302, 33001)])
 def test_backward_of_large_tiles(b, w, d, storage):
     backward_case(b, w, d, storage, b % 2)
 
