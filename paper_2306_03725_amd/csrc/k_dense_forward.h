@@ -229,7 +229,7 @@ k_dense_forward(Forward a) {
         }
         float x[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
+        for (int j = 0; j < N; ++j) x[j] = act_of<ACT, sizeof(TO) == 2>(v[0][j]) * v[MATS - 1][j];
         put_tile<TO, WD, sizeof(T) == 1>(mine, (TO*)a.x, x, i0 + g * 16, a.b, c0, a.d, past);
         if (a.gate) put_tile<TO, WD, true>(mine, (TO*)a.gate, v[0], i0 + g * 16, a.b, c0, a.d, past);
         if (a.up) put_tile<TO, WD, true>(mine, (TO*)a.up, v[MATS - 1], i0 + g * 16, a.b, c0, a.d, past);
@@ -293,7 +293,7 @@ k_dense_few(Forward a) {
         }
         float x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = act_of<ACT>(v[0][j]) * v[MATS - 1][j];
+        for (int j = 0; j < 4; ++j) x[j] = act_of<ACT, sizeof(TO) == 2>(v[0][j]) * v[MATS - 1][j];
         put_many((TO*)a.x + to, x, a.d - at);
         if (a.gate) put_many((TO*)a.gate + to, v[0], a.d - at);
         if (a.up) put_many((TO*)a.up + to, v[MATS - 1], a.d - at);
