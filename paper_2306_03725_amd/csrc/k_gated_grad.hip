@@ -329,7 +329,7 @@ k_gated_join(const float* __restrict__ sums, float* __restrict__ grad_e, size_t 
     if (wave == 0 && v < n) grad_e[v] = part[0][l] + part[1][l] + part[2][l] + part[3][l];
 }
 
-constexpr size_t SCRATCH = (size_t)1 << 30;   // what the chunk of instances is cut to, if 256 of them take less
+constexpr size_t SCRATCH = (size_t)1 << 30, CHUNK = 256;   // bytes that a chunk of instances is cut to, if CHUNK of them take less
 
 template <typename F>
 usl_status lds_for(usl_ctx* c, F* kernel, int bytes) {
@@ -391,12 +391,17 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
     const char* what = "gated_block_backward";
     a.dp = (a.d + 127) / 128 * 128;
     a.wp = a.w <= 128 ? 128 : (a.w + 255) / 256 * 256;
-    const size_t row = ((size_t)PARTS<T> * 2 * a.dp + a.wp) * ES;
+    // What an instance of a chunk takes: its rows of G and of e's copy; with grad_e's sums, if they are one piece
+    auto taken = [&](int w, int wp) { return ((size_t)PARTS<T> * 2 * a.dp + wp) * ES + (size_t)w * 4; };
     auto padded = [](size_t n) { return (n + 31) / 32 * 32; };   // a step of K, and more than a wavefront's rows
-    size_t most = padded((size_t)c->max_b);
-    if (most * row > SCRATCH) most = padded(SCRATCH / row < 256 ? 256 : SCRATCH / row);
-    if (most > padded((size_t)c->max_b)) most = padded((size_t)c->max_b);
-    if (most > 32768) most = 32768;   // a row is a grid dimension
+    const size_t row = taken(0, a.wp), each = taken(a.w, a.wp), all = padded((size_t)(c->max_b < 32768 ? c->max_b : 32768));   // a row is a grid dimension
+    auto smaller = [](size_t p, size_t q) { return p < q ? p : q; };
+    auto larger = [](size_t p, size_t q) { return p > q ? p : q; };
+    const size_t most = smaller(all, larger(SCRATCH / each / 32 * 32, CHUNK));
+    // Several pieces of grad_e's sums: no more tiles than compute units, of 128 x 256 at most
+    const size_t pieces = (size_t)c->num_cu * 128 * 256 * 4;
+    // Never less for a larger w, though the chunk is shorter: only a w larger than any before makes a call allocate
+    auto need = [&](size_t of) { return pieces + smaller(all * of, larger(SCRATCH, CHUNK * of)); };
     const int k_steps = 2 * a.dp / DEPTH;
     const uintptr_t rows_at = a.w * ES | (uintptr_t)a.V[0] | (uintptr_t)a.V[1];
     const int how = rows_at % 16 == 0 ? DIRECT : rows_at % 4 == 0 && a.w * ES >= 16 ? WORDS : REGISTERS;   // (16 bytes from a row on end in the next one at the latest)
@@ -410,9 +415,7 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         g.splits = (k_steps + g.steps_each - 1) / g.steps_each;
         return t;
     };
-    // pieces' sums: no more tiles than compute units, of 128 x 256 at most, or one piece of everything
-    const size_t by_tiles = (size_t)c->num_cu * 128 * 256, sums_most = by_tiles > most * a.w ? by_tiles : most * (size_t)a.w;
-    USL_TRY(usl_reserve_kept(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, most * row + sums_most * 4));
+    USL_TRY(usl_reserve_kept(c, (void**)&c->gated_scratch, &c->gated_scratch_cap, need(each), need(taken(65536, 65536))));
     a.G = c->gated_scratch;
     const char *e = (const char*)a.e, *gate = (const char*)a.gate, *up = (const char*)a.up;
     const float* grad_x = a.grad_x;

@@ -99,11 +99,11 @@ usl_status usl_reserve(usl_ctx* c, void** buf, size_t* cap, size_t bytes) {
     return USL_OK;
 }
 
-usl_status usl_reserve_kept(usl_ctx* c, void** buf, size_t* cap, size_t bytes) {
+usl_status usl_reserve_kept(usl_ctx* c, void** buf, size_t* cap, size_t bytes, size_t most) {
     if (*buf && *cap >= bytes) return USL_OK;
     const int room = (int)(sizeof(c->outgrown) / sizeof(c->outgrown[0]));
     if (*buf && c->outgrown_n == room) USL_FAIL(c, USL_ENOMEM, "scratch has grown %d times", room);
-    if (*buf && bytes < *cap + *cap / 2) bytes = *cap + *cap / 2;   // 32 times are enough for any need
+    if (*buf && bytes < *cap + *cap / 2) bytes = *cap + *cap / 2 < most ? *cap + *cap / 2 : most;   // 32 times are enough for any need
     void* grown = nullptr;
     hipError_t e = hipMalloc(&grown, bytes);
     if (e != hipSuccess) USL_FAIL(c, USL_ENOMEM, "hipMalloc of %zu bytes failed: %s", bytes, hipGetErrorString(e));

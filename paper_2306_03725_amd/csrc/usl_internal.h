@@ -131,8 +131,9 @@ struct usl_ctx {
 // Makes the device current on first use and reads its compute-unit count.
 usl_status usl_prepare_device(usl_ctx* ctx);
 // Grows *buf to at least `bytes` (old contents are dropped).
-usl_status usl_reserve_kept(usl_ctx* ctx, void** buf, size_t* cap, size_t bytes);   // the same for scratch whose need a call's arguments set: the old one lives on
 usl_status usl_reserve(usl_ctx* ctx, void** buf, size_t* cap, size_t bytes);
+// The same for scratch whose need a call's arguments set, `most` bytes for any of them: the old one lives on.
+usl_status usl_reserve_kept(usl_ctx* ctx, void** buf, size_t* cap, size_t bytes, size_t most);
 // The per-block loss sums of every loss kernel, for max_b instances: no later call has to grow them (growing frees and
 // allocates, which waits for the stream).  usl_forward_blocks: workgroups that forward may have when it sums the loss.
 usl_status usl_reserve_loss_partials(usl_ctx* ctx);
