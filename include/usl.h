@@ -301,7 +301,8 @@ usl_status usl_topk_adjusted(usl_ctx* ctx, const float* out, const usl_adjustmen
 
 /* ---- In front of the layer: the gated block that widens a trunk's output e to the activations x, and its products in 8-bit integers ----
  * (The paper feeds the layer from one dense "intermediate" layer of 16 to 65 thousand units; the block has two, the second gated by the first.)
- * e [b][w] storage type, the trunk's output; V_gate, V_up [d][w] storage type.  1 <= w <= 65536, d <= 2^20 (else USL_ESHAPE).
+ * e [b][w] storage type, the trunk's output; V_gate, V_up [d][w] storage type, in float32 at multiples of 4 bytes (else USL_EINVAL).  1 <= w <= 65536,
+ * d <= 2^20 (else USL_ESHAPE).
  * act: what the gate goes through, USL_SILU a / (1 + exp(-a)) or USL_GELU a * Phi(a), Phi the standard normal distribution's function. */
 typedef enum { USL_SILU = 0, USL_GELU = 1 } usl_act;
 

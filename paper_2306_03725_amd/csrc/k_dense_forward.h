@@ -312,6 +312,14 @@ usl_status launch_tiles(usl_ctx* c, Forward a, const char* what) {
     return usl_check_launch(c, what);
 }
 
+template <typename T, typename TO, int MATS, int ACT, int BD, int BB, int STAGES>
+usl_status launch_any(usl_ctx* c, const Forward& a, const char* what, int how) {
+    if (how == DIRECT) return launch_tiles<T, TO, MATS, ACT, BD, BB, 2, 2, STAGES, DIRECT>(c, a, what);
+    if constexpr (sizeof(T) < 4)   // (float32 numbers lie at multiples of 4 bytes)
+        if (how == REGISTERS) return launch_tiles<T, TO, MATS, ACT, BD, BB, 2, 2, 2, REGISTERS>(c, a, what);
+    return launch_tiles<T, TO, MATS, ACT, BD, BB, 2, 2, STAGES, WORDS>(c, a, what);
+}
+
 // Which tiles?  A compute unit's time is that of the tiles that fall to it, whole ones of them, each as long as its area over its rate: large ones read fragments less often
 // (in float32 the matrix cores are so slow that it does not matter), small ones leave less undone at the edges and fall to the compute units more evenly.  Rates from
 // 512 x 768 -> 32768 (bfloat16 128 x 256 67 us, 128 x 128 83, 64 x 64 114, 32 x 64 160).  us, gated, w = 768, bfloat16 if not said otherwise, by what the rule takes and by others:
@@ -344,18 +352,10 @@ usl_status launch_forward(usl_ctx* c, Forward a, const char* what) {
                  by_32 = MATS == 2 ? cost(32, 64, SLOW ? 0.9 : 0.42) : INFINITY;
     if (by_many <= by_128 && by_many <= by_64 && by_many <= by_32)
         return how == DIRECT ? launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, DIRECT>(c, a, what) : launch_tiles<T, TO, MATS, ACT, MANY, 256, 2, 4, 4, WORDS>(c, a, what);
-    if (by_128 <= by_64 && by_128 <= by_32)
-        return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, DIRECT>(c, a, what)
-               : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 3, WORDS>(c, a, what)
-                              : launch_tiles<T, TO, MATS, ACT, 128, 128, 2, 2, 2, REGISTERS>(c, a, what);
+    if (by_128 <= by_64 && by_128 <= by_32) return launch_any<T, TO, MATS, ACT, 128, 128, 3>(c, a, what, how);
     if constexpr (MATS == 2)
-        if (by_32 < by_64)
-            return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, DIRECT>(c, a, what)
-                   : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 4, WORDS>(c, a, what)
-                                  : launch_tiles<T, TO, MATS, ACT, 32, 64, 2, 2, 2, REGISTERS>(c, a, what);
-    return how == DIRECT  ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, DIRECT>(c, a, what)
-           : how == WORDS ? launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 4, WORDS>(c, a, what)
-                          : launch_tiles<T, TO, MATS, ACT, 64, 64, 2, 2, 2, REGISTERS>(c, a, what);
+        if (by_32 < by_64) return launch_any<T, TO, MATS, ACT, 32, 64, 4>(c, a, what, how);
+    return launch_any<T, TO, MATS, ACT, 64, 64, 4>(c, a, what, how);
 }
 
 }  // namespace dense

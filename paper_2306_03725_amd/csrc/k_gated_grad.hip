@@ -357,7 +357,9 @@ usl_status grad_e_tiles(usl_ctx* c, const Grad& a) {
 template <typename T, int MT, int NT, int FN>
 usl_status grad_e(usl_ctx* c, const Grad& a, int how) {
     if (how == DIRECT) return grad_e_tiles<T, MT, NT, FN, 4, DIRECT>(c, a);
-    return how == WORDS ? grad_e_tiles<T, MT, NT, FN, 4, WORDS>(c, a) : grad_e_tiles<T, MT, NT, FN, 3, REGISTERS>(c, a);
+    if constexpr (sizeof(T) == 2 || MT == 128)   // (rows of float32 are rows of words, but for those below 16 bytes)
+        if (how == REGISTERS) return grad_e_tiles<T, MT, NT, FN, 3, REGISTERS>(c, a);
+    return grad_e_tiles<T, MT, NT, FN, 4, WORDS>(c, a);
 }
 
 // Tiles of grad_e.  Instances 32 or 64 at a time where there are no more, and 64 where V comes straight into LDS and they leave out an eighth of what 128 at a time
@@ -434,8 +436,10 @@ usl_status run(usl_ctx* c, Grad a, int32_t act, int32_t b) {
         else hipLaunchKernelGGL((k_gated_slopes<T, 1>), slopes, dim3(PREP_NT), 0, c->stream, a);
         USL_TRY(usl_check_launch(c, what));
         if (a.grad_V[0] || a.grad_V[1]) {
-            if (tall_v<T>(c, a.w, a.dp)) USL_TRY((grad_v<T, 256, 128, 4, 4>(c, a)));
-            else USL_TRY((grad_v<T, 64, 64, 2, 4>(c, a)));
+            const bool tall = tall_v<T>(c, a.w, a.dp);
+            if constexpr (ES == 2)
+                if (tall) USL_TRY((grad_v<T, 256, 128, 4, 4>(c, a)));
+            if (!tall) USL_TRY((grad_v<T, 64, 64, 2, 4>(c, a)));
         }
         if (!a.grad_e) continue;
         const Tiles t = cut(a, a.rows);

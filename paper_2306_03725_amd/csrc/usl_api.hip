@@ -606,6 +606,11 @@ static usl_status check_block(usl_ctx* c, int32_t w) {
     if (c->d > 1 << 20) USL_FAIL(c, USL_ESHAPE, "d = %d, the dense calls take at most 2^20", c->d);
     return USL_OK;
 }
+// Rows of float32 go to LDS in words
+static usl_status check_words(usl_ctx* c, const void* e, const void* V_gate, const void* V_up) {
+    if (c->storage == USL_F32 && ((uintptr_t)e | (uintptr_t)V_gate | (uintptr_t)V_up) % 4) USL_FAIL(c, USL_EINVAL, "e, V_gate and V_up must lie at multiples of 4 bytes");
+    return USL_OK;
+}
 static usl_status check_act(usl_ctx* c, int32_t act) {
     if (act != USL_SILU && act != USL_GELU) USL_FAIL(c, USL_EINVAL, "act %d is neither USL_SILU nor USL_GELU", act);
     return USL_OK;
@@ -629,6 +634,7 @@ extern "C" usl_status usl_gated_block(usl_ctx* c, const void* e, const void* V_g
     USL_TRY(check_batch(c, b));
     USL_TRY(check_block(c, w));
     USL_TRY(check_act(c, act));
+    USL_TRY(check_words(c, e, V_gate, V_up));
     const void *results[] = {x, gate, up}, *inputs[] = {e, V_gate, V_up};
     USL_TRY(check_apart(c, results, 3, inputs, 3));
     USL_TRY(usl_prepare_device(c));
@@ -642,6 +648,7 @@ extern "C" usl_status usl_gated_block_backward(usl_ctx* c, const float* grad_x, 
     USL_TRY(check_batch(c, b));
     USL_TRY(check_block(c, w));
     USL_TRY(check_act(c, act));
+    USL_TRY(check_words(c, e, V_gate, V_up));
     const void *results[] = {grad_e, grad_V_gate, grad_V_up}, *inputs[] = {grad_x, e, V_gate, V_up, gate, up};
     USL_TRY(check_apart(c, results, 3, inputs, 6));
     if (!grad_e && !grad_V_gate && !grad_V_up) return USL_OK;
