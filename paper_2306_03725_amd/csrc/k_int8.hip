@@ -7,6 +7,7 @@ using namespace dense;
 namespace {
 
 constexpr int Q_NT = 256;
+constexpr int64_t Q_ROWS = 1 << 22;   // of a launch: it takes less than 2^32 work items
 
 // A row to a workgroup: the largest magnitude, then the codes.  scale = max(largest / 127, 2^-126); code = value / scale to the nearest, halves to even.
 // A row with an infinity or NaN has NaN as its scale, and codes 0.
@@ -42,10 +43,16 @@ usl_status product(usl_ctx* c, const Forward& a, int mats, int act, const char* 
 }  // namespace
 
 usl_status usl_launch_quantize_i8(usl_ctx* c, const void* rows, int64_t n, int32_t w, int8_t* codes, float* scales) {
-    const dim3 grid((unsigned)n), block(Q_NT);
-    if (c->storage == USL_F32) hipLaunchKernelGGL(k_quantize_i8<float>, grid, block, 0, c->stream, (const float*)rows, (int)w, codes, scales);
-    else hipLaunchKernelGGL(k_quantize_i8<bf16>, grid, block, 0, c->stream, (const bf16*)rows, (int)w, codes, scales);
-    return usl_check_launch(c, "quantize_i8");
+    const size_t wide = c->storage == USL_F32 ? 4 : 2;
+    for (int64_t at = 0; at < n; at += Q_ROWS) {
+        const void* from = (const char*)rows + (size_t)at * (size_t)w * wide;
+        int8_t* to = codes + (size_t)at * (size_t)w;
+        const dim3 grid((unsigned)(n - at < Q_ROWS ? n - at : Q_ROWS)), block(Q_NT);
+        if (c->storage == USL_F32) hipLaunchKernelGGL(k_quantize_i8<float>, grid, block, 0, c->stream, (const float*)from, (int)w, to, scales + at);
+        else hipLaunchKernelGGL(k_quantize_i8<bf16>, grid, block, 0, c->stream, (const bf16*)from, (int)w, to, scales + at);
+        USL_TRY(usl_check_launch(c, "quantize_i8"));
+    }
+    return USL_OK;
 }
 
 usl_status usl_launch_dense_i8(usl_ctx* c, const int8_t* e, const float* e_scales, const int8_t* V0, const float* s0, const int8_t* V1, const float* s1, int32_t w,
