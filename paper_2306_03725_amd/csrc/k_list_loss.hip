@@ -255,13 +255,18 @@ k_list_loss(Lists a, const double* __restrict__ row_loss) {
     add_losses(a, row_loss, red);
 }
 
-// g may be out: a segment's scores and its entries' are read before a barrier, and g is written behind it.
-// Several entries of one label are added up by the first of them, in the list's order.
+// g may be out: a lane writes where it has read, and its segment's entries' scores are read before a barrier, and g is written behind it.
+// A label with one entry takes its value from that entry.  Those of several are added up in the list's order, LL_NT entries at a time, by the first entry of the label among
+// them: a list of n entries costs n steps, whatever it repeats.  (The first entry of all walking the rest of the list alone: one row of 20000 entries in far pairs, 30938 labels, 37 ms, so 0.67; 64 rows, 500k labels, 177 and 4.0.)
 template <bool TEACHER>
 __global__ void __launch_bounds__(LL_NT)
 k_list_grad(Lists a, const Row* __restrict__ rows, const double* __restrict__ row_loss, float* g) {
     __shared__ __align__(16) uint32_t first[LL_SEG];   // the first entry of a label
-    __shared__ __align__(16) uint32_t more[LL_SEG];    // how many it has; then the bits of their sum
+    __shared__ __align__(16) uint32_t more[LL_SEG];    // how many it has; then the bits of their sum (in between, with first: of the sum in float64)
+    __shared__ uint32_t repeated[LL_SEG / 32];         // labels of several entries
+    __shared__ int some;                               // whether there are any
+    __shared__ __align__(16) int32_t turn_lab[LL_NT];  // of LL_NT entries: those of such labels, else -1
+    __shared__ double turn_c[LL_NT];
     __shared__ double red[LL_NT / 64];
     if (blockIdx.x == 0 && blockIdx.y == 0) add_losses(a, row_loss, red);
     const int i = (int)blockIdx.y, tid = (int)threadIdx.x;
@@ -290,6 +295,8 @@ k_list_grad(Lists a, const Row* __restrict__ rows, const double* __restrict__ ro
                 reinterpret_cast<uint4*>(first)[e * LL_NT + tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
                 reinterpret_cast<uint4*>(more)[e * LL_NT + tid] = make_uint4(0, 0, 0, 0);
             }
+            if (tid < LL_SEG / 32) repeated[tid] = 0;
+            if (tid == 0) some = 0;
             __syncthreads();
             for (int64_t p = tid; p < n; p += LL_NT) {
                 const int32_t label = a.lab[p0 + p];
@@ -303,17 +310,51 @@ k_list_grad(Lists a, const Row* __restrict__ rows, const double* __restrict__ ro
                 const int32_t label = a.lab[p0 + p];
                 const uint32_t j = (uint32_t)label - (uint32_t)seg0;
                 if (!here(label) || first[j] != (uint32_t)p) continue;
-                double c = slope(p0 + p);
-                uint32_t left = more[j] - 1;
-                for (int64_t u = p + 1; left; ++u)
-                    if (a.lab[p0 + u] == label) {
-                        c += slope(p0 + u);
-                        --left;
+                if (more[j] == 1) more[j] = __float_as_uint((float)(a.scale * slope(p0 + p)));
+                else {
+                    atomicOr(&repeated[j >> 5], 1u << (j & 31));
+                    some = 1;
+                }
+            }
+            __syncthreads();
+            if (some) {
+                auto is = [&](uint32_t j) { return repeated[j >> 5] >> (j & 31) & 1u; };
+                for (uint32_t j = tid; j < LL_SEG; j += LL_NT)
+                    if (is(j)) first[j] = more[j] = 0;   // 0.0
+                for (int64_t base = 0; base < n; base += LL_NT) {
+                    const int32_t label = base + tid < n ? a.lab[p0 + base + tid] : -1;
+                    const uint32_t j = (uint32_t)label - (uint32_t)seg0;
+                    const bool own = here(label) && is(j);
+                    turn_lab[tid] = own ? label : -1;
+                    if (own) turn_c[tid] = slope(p0 + base + tid);
+                    if (__syncthreads_or(own)) {
+                        if (own) {
+                            double c = __longlong_as_double((long long)((uint64_t)more[j] << 32 | first[j]));
+                            bool lead = true;
+#pragma unroll 4
+                            for (int t = 0; t < LL_NT; t += 4) {
+                                const int4 q = *reinterpret_cast<const int4*>(turn_lab + t);
+                                const int same = (q.x == label) | (q.y == label) << 1 | (q.z == label) << 2 | (q.w == label) << 3;
+                                if (!same) continue;
+                                for (int u = 0; u < 4; ++u)
+                                    if (same >> u & 1) {
+                                        lead = lead && t + u >= tid;
+                                        c += turn_c[t + u];
+                                    }
+                            }
+                            if (lead) {
+                                first[j] = (uint32_t)(uint64_t)__double_as_longlong(c);
+                                more[j] = (uint32_t)((uint64_t)__double_as_longlong(c) >> 32);
+                            }
+                        }
+                        __syncthreads();
                     }
-                more[j] = __float_as_uint((float)(a.scale * c));
+                }
+                for (uint32_t j = tid; j < LL_SEG; j += LL_NT)
+                    if (is(j)) more[j] = __float_as_uint((float)(a.scale * __longlong_as_double((long long)((uint64_t)more[j] << 32 | first[j]))));
+                __syncthreads();
             }
         }
-        __syncthreads();
 #pragma unroll
         for (int e = 0; e < LL_EPT; e += 4) {
             float c[4] = {0.f, 0.f, 0.f, 0.f};
