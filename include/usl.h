@@ -318,7 +318,8 @@ usl_status usl_gated_block(usl_ctx* ctx, const void* e, const void* V_gate, cons
  *   G_gate = grad_x * up * act'(gate),  G_up = grad_x * act(gate)
  *   grad_e = G_gate V_gate + G_up V_up [b][w],  grad_V_gate = G_gate^T e,  grad_V_up = G_up^T e [d][w]
  * e, V_gate, V_up as the forward call had them, gate and up as it left them.  grad_x and the results are float32, overwritten; each result may be
- * NULL, and none may be an input or another result.  Everything is computed in float32.  Where e, a matrix or G holds an infinity, the sums that it enters
+ * NULL, and none may be an input or another result.  Everything is computed in float32 (with bfloat16 storage without
+ * what G holds below 2^-126, which is less than a rounding where G is of 2^-105 and more).  Where e, a matrix or G holds an infinity, the sums that it enters
  * are infinite or NaN.  Sums are taken in a fixed order: equal calls give equal bits.  Scratch is sized for max_b and w; a call with a larger w than any before
  * allocates (what it had is kept until usl_destroy, for graphs that were captured with it). */
 usl_status usl_gated_block_backward(usl_ctx* ctx, const float* grad_x, const void* e, const void* V_gate, const void* V_up, const void* gate,
